@@ -108,6 +108,58 @@ dfq_status dfq_dequantize(const int8_t *q, float *x, size_t n, dfq_fmt fmt, dfq_
 dfq_status dfq_quantize_np(const float *x, uint8_t *codes, size_t n, int nbits, int p, int frac, dfq_stream stream);
 dfq_status dfq_dequantize_np(const uint8_t *codes, float *x, size_t n, int nbits, int p, int frac, dfq_stream stream);
 
+/* ---- microscaled tensors: 4- and 8-bit elements with one power-of-two scale for 32 values ---------------
+ * A row of K >= 1 values is ceil(K / 32) blocks of 32 consecutive ones (the last may be short).  An element is
+ *   DFQ_MX4  E2M1, two to a byte, the even one in the low half: the (4, 1) code of Eq. 2 at alpha = 1/2, magnitudes 0 .5 1 1.5 2 3 4 6
+ *   DFQ_MX8  E4M3, one to a byte: the (8, 3) code of Eq. 2 at alpha = 2^-9, up to 448; 0x7f and 0xff are NaN
+ * and the value it stands for is element * 2^(s - 127) with s the block's scale byte; s = 255: every value of the block is NaN.
+ * Row r's codes start at codes + r * ldc: ceil(K / 32) * 16 bytes (DFQ_MX4) or * 32 (DFQ_MX8), zeros behind K; codes 16-byte
+ * aligned, ldc a multiple of 16 and at least that many.  Its scales start at scales + r * lds; scales 4-byte aligned, lds a
+ * multiple of 4 and at least ceil(K / 32); the bytes from there to the next multiple of 4 are padding, written as zeros and read
+ * without effect.  Floating-point rows are `ld` ELEMENTS of `dtype` apart, ld >= K, aligned to their type.  Every call takes rows of
+ * up to 2^22 values and up to 2^31 - 1 rows (DFQ_EUNSUPPORTED beyond); rows == 0 (M == 0) is a no-op.  Everything DEVICE.
+ *
+ * The exponent e = s - 127 of a block with largest magnitude amax, top the largest element (6 or 448):
+ *   DFQ_MX_COVER  the smallest e with amax <= top * 2^e (the rule of dfq_fmt_from_absmax_f32: the largest value is never clipped)
+ *   DFQ_MX_FLOOR  floor(log2 amax) - floor(log2 top): magnitudes above top * 2^e saturate
+ * never below -127, which is also the exponent of a block of zeros.  Each value is divided by 2^e and rounded to the nearest element,
+ * ties to the even code, saturating; the code of -0 is never written.  A block that holds an infinity or a NaN becomes s = 255 with
+ * zero codes: a NaN is not lost, and a product that reads the block is NaN. */
+typedef enum { DFQ_F32 = 0, DFQ_BF16 = 1, DFQ_F16 = 2 } dfq_dtype;
+typedef enum { DFQ_MX4 = 0, DFQ_MX8 = 1 } dfq_mx_elem;
+typedef enum { DFQ_MX_COVER = 0, DFQ_MX_FLOOR = 1 } dfq_mx_rule;
+
+dfq_status dfq_quantize_mx(const void *x, size_t ldx, dfq_dtype dtype, size_t rows, int K, uint8_t *codes, size_t ldc, uint8_t *scales,
+                           size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, dfq_stream stream);
+
+/* The values, rounded once to dtype (exact in float32; in bfloat16 down to 2^-133). */
+dfq_status dfq_dequantize_mx(const uint8_t *codes, size_t ldc, const uint8_t *scales, size_t lds, dfq_mx_elem elem, size_t rows, int K,
+                             void *x, size_t ldx, dfq_dtype dtype, dfq_stream stream);
+
+/* y[m][n] = sum_k x[m][k] * w[n][k] + bias[n] (bias: N floats or NULL), with relu max(., 0), rounded once to dtype.
+ * x: M rows of K, w: N rows of K, both microscaled and each with its own elements; y: M rows of N, ldy elements apart.
+ * Products and sums are float32's for float32 results and for 4-bit operands.  For 16-bit and converted results of 8-bit operands
+ * the products of eight consecutive k are aligned to the largest of them, 13 bits behind its leading one, before they enter the
+ * float32 sum: far below the rounding of the result unless the sum cancels.  Sums below 2^-126 may become 0. */
+dfq_status dfq_linear_mx(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
+                         const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, void *y, size_t ldy, dfq_dtype dtype,
+                         size_t M, int N, int K, int relu, dfq_stream stream);
+
+/* The same with the float32 results converted to a microscaled tensor of M rows of N by the rule above, without a rounding between:
+ * what the next product reads. */
+dfq_status dfq_linear_mx_q(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
+                           const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, uint8_t *codes, size_t ldc,
+                           uint8_t *scales, size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream);
+
+/* Root-mean-square norm with the addition in front of it and the conversion behind it, row by row, in float32:
+ *   s = x + add;  v = s / sqrt(mean(s^2) + eps) * weight;  sum = s rounded to dtype;  y = v rounded to dtype;  codes, scales = v converted
+ * add, sum, weight (NULL: ones), y and codes may be NULL, y and codes not both; the norm reads s unrounded.  x, add, sum and y are rows
+ * of dtype, weight K values of wtype, which is dtype or DFQ_F32.  sum may be x or add (same address and row distance): the residual
+ * stream is then updated in place.  eps >= 0 and finite; a row of zeros with eps = 0 is NaN. */
+dfq_status dfq_rms_norm_mx(const void *x, size_t ldx, const void *add, size_t ldadd, void *sum, size_t ldsum, dfq_dtype dtype,
+                           const void *weight, dfq_dtype wtype, float eps, void *y, size_t ldy, uint8_t *codes, size_t ldc, uint8_t *scales,
+                           size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t rows, int K, dfq_stream stream);
+
 /* ---- convolution / inner product (Sec. 2.2, Eq. 6) -------------------------------------
  * acc[n,p,q,k] = sum_{r,s,c} x[n, p*stride-pad+r, q*stride-pad+s, g*Cg+c] * w[k,r,s,c] + b[k]
  * with Cg = C/groups, g = k / (K/groups); taps outside the image contribute 0.
@@ -492,7 +544,8 @@ dfq_status dfq_cal_add_np(const int8_t *ah, const int8_t *al, const int32_t *fra
 /* ---- A pass as one call ----------------------------------------------------------------------
  * A plan is a fixed sequence of calls; issued one by one from a scripting language their marshalling costs more than their
  * launches.  A record holds a call's number (dfq_call_number of the function's name, HOST; -1 for one that is no stream
- * call) and its arguments but the stream in order, each as 64 bits: integers, pointers as numbers, a dfq_fmt by its fractional length.
+ * call) and its arguments but the stream in order, each as 64 bits: integers, pointers as numbers, a dfq_fmt by its fractional length,
+ * a float by its 32 bits.
  * dfq_run_calls makes the calls in order on the stream and stops at the first that is refused: its status is returned and
  * its index stored in *failed (may be null).  DFQ_EINVAL for a record with an unknown number or a wrong count of arguments. */
 #define DFQ_CALL_ARGS 30

@@ -8,8 +8,10 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from array import array
-from typing import Optional, Sequence
+from contextlib import nullcontext
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -18,6 +20,9 @@ LIB_PATH = os.path.join(_HERE, "libdfq.so")
 
 OK, EINVAL, ESHAPE, EFMT, EUNSUPPORTED, EDEVICE = range(6)
 POOL_MAX, POOL_AVG = 0, 1
+MX4, MX8 = 0, 1               # dfq_mx_elem
+MX_COVER, MX_FLOOR = 0, 1     # dfq_mx_rule
+MX_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # dfq_dtype
 CAL_AMAX_WORDS = 256          # DFQ_CAL_AMAX_WORDS
 CALL_ARGS = 30                # DFQ_CALL_ARGS
 CONV_AUTO, CONV_DIRECT, CONV_MFMA, CONV_DEPTHWISE, CONV_SMALLC, CONV_POINTWISE, CONV_GROUPED, CONV_RAGGED, CONV_SPLIT = range(9)
@@ -35,6 +40,7 @@ EXPORTS = [
     "dfq_cal_weights", "dfq_cal_quantize", "dfq_cal_rescale", "dfq_cal_add", "dfq_cal_concat",
     "dfq_cal_np_weights", "dfq_cal_np_quantize", "dfq_cal_conv_np", "dfq_cal_add_np",
     "dfq_conv_np_absmax", "dfq_eltwise_np_absmax", "dfq_np_frac_from_absmax_u64", "dfq_pool_np", "dfq_stem_pack_x", "dfq_stem_pack_w", "dfq_conv_np_add",
+    "dfq_quantize_mx", "dfq_dequantize_mx", "dfq_linear_mx", "dfq_linear_mx_q", "dfq_rms_norm_mx",
     "dfq_conv_q_maxpool", "dfq_quantize_conv_q_maxpool", "dfq_conv_q_pc_maxpool", "dfq_quantize_conv_q_pc_maxpool", "dfq_quantize_conv_q",
 ]
 
@@ -146,6 +152,14 @@ def lib():
     L.dfq_cal_add_np.argtypes = [vp] * 6 + [sz, i32, i32] + [vp] * 6
     for name in ("dfq_cal_weights", "dfq_cal_quantize", "dfq_cal_rescale", "dfq_cal_add", "dfq_cal_concat", "dfq_cal_np_weights", "dfq_cal_np_quantize", "dfq_cal_conv_np", "dfq_cal_add_np"):
         getattr(L, name).restype = i32
+    L.dfq_quantize_mx.argtypes = [vp, sz, i32, sz, i32, vp, sz, vp, sz, i32, i32, vp]
+    L.dfq_dequantize_mx.argtypes = [vp, sz, vp, sz, i32, sz, i32, vp, sz, i32, vp]
+    linear_args = [vp, sz, vp, sz, i32] * 2 + [vp]
+    L.dfq_linear_mx.argtypes = linear_args + [vp, sz, i32, sz, i32, i32, i32, vp]
+    L.dfq_linear_mx_q.argtypes = linear_args + [vp, sz, vp, sz, i32, i32, sz, i32, i32, i32, vp]
+    L.dfq_rms_norm_mx.argtypes = [vp, sz, vp, sz, vp, sz, i32, vp, i32, C.c_float, vp, sz, vp, sz, vp, sz, i32, i32, sz, i32, vp]
+    for name in ("dfq_quantize_mx", "dfq_dequantize_mx", "dfq_linear_mx", "dfq_linear_mx_q", "dfq_rms_norm_mx"):
+        getattr(L, name).restype = i32
     L.dfq_hist_shift.argtypes = [i64]
     L.dfq_hist_shift.restype = i32
     for name in ("dfq_quantize", "dfq_quantize_i32", "dfq_dequantize", "dfq_conv_q", "dfq_conv_q_variant",
@@ -226,8 +240,8 @@ class CallList:
             if number is None:
                 number = self._numbers[name] = lib().dfq_call_number(name.encode())
             words.append((number & 0xffffffff) | len(args) << 32)
-            words += [a if type(a) is int else a.frac if type(a) is Fmt else 0 if a is None else of_array(a) if isinstance(a, C.Array) else int(a)
-                      for a in args]
+            words += [a if type(a) is int else a.frac if type(a) is Fmt else 0 if a is None else of_array(a) if isinstance(a, C.Array) else
+                      struct.unpack("<I", struct.pack("<f", a))[0] if type(a) is float else int(a) for a in args]
             words += _ZEROS[len(args):]
         self._held, self._count = calls, len(calls)
         self._input, self._arrays, self._at = input_ptr, arrays, None
@@ -311,6 +325,169 @@ def dequantize_np(q: torch.Tensor, nbits: int, p: int, frac: int, out: Optional[
     x = out if out is not None else torch.empty(q.shape, dtype=torch.float32, device=q.device)
     _check(lib().dfq_dequantize_np(_ptr(q), _ptr(x), q.numel(), int(nbits), int(p), int(frac), _stream(stream)), "dfq_dequantize_np")
     return x
+
+
+# ---- microscaled tensors ---------------------------------------------------------- #
+class MxTensor(NamedTuple):
+    """Rows of k values as 4- or 8-bit elements with one power-of-two scale for 32 of them (include/dfq.h).  codes: uint8 [rows, bytes], scales:
+    uint8 [rows, a multiple of 4], the columns behind ceil(k / 32) padding; both may be slices of wider rows."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    elem: int
+    k: int
+
+    @classmethod
+    def empty(cls, rows: int, k: int, elem: int, device="cuda") -> "MxTensor":
+        nb = (k + 31) // 32
+        return cls(torch.empty((rows, nb * (32 if elem == MX8 else 16)), dtype=torch.uint8, device=device),
+                   torch.empty((rows, (nb + 3) // 4 * 4), dtype=torch.uint8, device=device), elem, k)
+
+
+def _here(t: torch.Tensor, name: str):
+    """A launch goes to the current device."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device")
+
+
+def _rows(t: torch.Tensor, name: str, dtype=None):
+    """[rows, k] with whole rows, or a contiguous tensor of more dimensions as its rows."""
+    _here(t, name)
+    if (t.dtype is not dtype) if dtype is not None else t.dtype not in MX_DTYPES:
+        raise TypeError(f"{name}: expected {dtype or 'float32, bfloat16 or float16'}")
+    if t.dim() != 2:
+        if t.dim() == 0 or not t.is_contiguous():
+            raise ValueError(f"{name}: expected [rows, k] or a contiguous tensor")
+        t = t.view(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row have to be next to each other")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _mx(q: MxTensor, name: str, rows: Optional[int] = None, k: Optional[int] = None):
+    """Checks a microscaled tensor; returns (codes, their row distance, scales, their row distance)."""
+    c, s = q.codes, q.scales
+    for t, what in ((c, "codes"), (s, "scales")):
+        _rows(t, f"{name}.{what}", torch.uint8)
+        if t.dim() != 2:
+            raise ValueError(f"{name}.{what}: expected [rows, bytes]")
+    if q.elem not in (MX4, MX8) or q.k < 1:
+        raise ValueError(f"{name}: no such element, or no values")
+    nb = (q.k + 31) // 32
+    if c.shape[0] != s.shape[0] or c.shape[1] < nb * (32 if q.elem == MX8 else 16) or s.shape[1] < (nb + 3) // 4 * 4:
+        raise ValueError(f"{name}: codes and scales do not hold rows of {q.k} values")
+    if (rows is not None and c.shape[0] != rows) or (k is not None and q.k != k):
+        raise ValueError(f"{name}: expected {rows if rows is not None else c.shape[0]} rows of {k if k is not None else q.k} values")
+    return c.data_ptr(), _ld(c), s.data_ptr(), _ld(s)
+
+
+def _allocating_on(stream):
+    """New tensors belong to the stream that writes them."""
+    if stream is None:
+        return nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+
+
+def quantize_mx(x: torch.Tensor, elem: int = MX8, rule: int = MX_COVER, out: Optional[MxTensor] = None, stream=None) -> MxTensor:
+    """float32, bfloat16 or float16 rows -> microscaled ones; the rows of a tensor of more dimensions are its last one's."""
+    x = _rows(x, "x")
+    rows, k = x.shape
+    if out is None:
+        with _allocating_on(stream):
+            out = MxTensor.empty(rows, k, elem, x.device)
+    elif out.elem != elem:
+        raise ValueError("out: holds other elements")
+    c, ldc, s, lds = _mx(out, "out", rows, k)
+    _check(lib().dfq_quantize_mx(x.data_ptr(), _ld(x), MX_DTYPES[x.dtype], rows, k, c, ldc, s, lds, int(elem), int(rule), _stream(stream)), "dfq_quantize_mx")
+    return out
+
+
+def dequantize_mx(q: MxTensor, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values of a microscaled tensor, [rows, k]."""
+    c, ldc, s, lds = _mx(q, "q")
+    rows = q.codes.shape[0]
+    if out is None:
+        with _allocating_on(stream):
+            out = torch.empty((rows, q.k), dtype=dtype, device=q.codes.device)
+    x = _rows(out, "out", dtype)
+    if dtype not in MX_DTYPES or x.shape != (rows, q.k):
+        raise ValueError(f"out: expected [{rows}, {q.k}] of float32, bfloat16 or float16")
+    _check(lib().dfq_dequantize_mx(c, ldc, s, lds, q.elem, rows, q.k, x.data_ptr(), _ld(x), MX_DTYPES[dtype], _stream(stream)), "dfq_dequantize_mx")
+    return out
+
+
+def _linear_operands(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor]):
+    xa, wa = _mx(x, "x"), _mx(w, "w", None, x.k)
+    n = w.codes.shape[0]
+    if bias is not None:
+        _here(bias, "bias")
+        if bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous():
+            raise ValueError(f"bias: expected {n} contiguous float32 values")
+    return x.codes.shape[0], n, (*xa, x.elem, *wa, w.elem, _ptr(bias))
+
+
+def linear_mx(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, relu: bool = False, dtype: torch.dtype = torch.bfloat16,
+              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x [m, k] times w [n, k] transposed, plus bias [n] float32, with relu max(., 0): [m, n] of dtype."""
+    m, n, operands = _linear_operands(x, w, bias)
+    if out is None:
+        with _allocating_on(stream):
+            out = torch.empty((m, n), dtype=dtype, device=x.codes.device)
+    y = _rows(out, "out", dtype)
+    if dtype not in MX_DTYPES or y.shape != (m, n):
+        raise ValueError(f"out: expected [{m}, {n}] of float32, bfloat16 or float16")
+    _check(lib().dfq_linear_mx(*operands, y.data_ptr(), _ld(y), MX_DTYPES[dtype], m, n, x.k, int(bool(relu)), _stream(stream)), "dfq_linear_mx")
+    return out
+
+
+def linear_mx_q(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, elem: int = MX8, rule: int = MX_COVER, relu: bool = False,
+                out: Optional[MxTensor] = None, stream=None) -> MxTensor:
+    """The same with the result converted for the next product."""
+    m, n, operands = _linear_operands(x, w, bias)
+    if out is None:
+        with _allocating_on(stream):
+            out = MxTensor.empty(m, n, elem, x.codes.device)
+    elif out.elem != elem:
+        raise ValueError("out: holds other elements")
+    _check(lib().dfq_linear_mx_q(*operands, *_mx(out, "out", m, n), int(elem), int(rule), m, n, x.k, int(bool(relu)), _stream(stream)), "dfq_linear_mx_q")
+    return out
+
+
+def rms_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6, add: Optional[torch.Tensor] = None,
+                elem: Optional[int] = MX8, rule: int = MX_COVER, want_y: bool = False, out: Optional[MxTensor] = None,
+                sum_out: Optional[torch.Tensor] = None, stream=None):
+    """Root-mean-square norm of the rows of x + add, times weight [k] (of x's type or float32), in float32.  Returns (the result converted, or
+    None for elem=None; the result in x's type with want_y, else None; x + add in x's type, None without add).  sum_out may be x or add."""
+    xr = _rows(x, "x")
+    rows, k = xr.shape
+    dt = x.dtype
+    ar = None if add is None else _rows(add, "add", dt)
+    if ar is not None and ar.shape != xr.shape:
+        raise ValueError("x and add do not match")
+    if weight is not None:
+        _here(weight, "weight")
+        if weight.dtype not in (dt, torch.float32) or weight.shape != (k,) or not weight.is_contiguous():
+            raise ValueError(f"weight: expected {k} contiguous values of x's type or float32")
+    with _allocating_on(stream):
+        if elem is not None and out is None:
+            out = MxTensor.empty(rows, k, elem, x.device)
+        y = torch.empty(x.shape, dtype=dt, device=x.device) if want_y else None
+        total = sum_out if sum_out is not None else torch.empty(x.shape, dtype=dt, device=x.device) if add is not None else None
+    if out is not None and out.elem != elem:
+        raise ValueError("out: holds other elements")
+    sr = None if total is None else _rows(total, "sum_out", dt)
+    if sr is not None and sr.shape != xr.shape:
+        raise ValueError("sum_out: expected the rows of x")
+    q = (None, 0, None, 0) if out is None else _mx(out, "out", rows, k)
+    _check(lib().dfq_rms_norm_mx(xr.data_ptr(), _ld(xr), _ptr(ar), 0 if ar is None else _ld(ar), _ptr(sr), 0 if sr is None else _ld(sr), MX_DTYPES[dt],
+                                 _ptr(weight), MX_DTYPES[dt if weight is None else weight.dtype], float(eps), _ptr(y), k, *q,
+                                 MX8 if elem is None else int(elem), int(rule), rows, k, _stream(stream)), "dfq_rms_norm_mx")
+    return out, y, total
 
 
 def np_digits(codes: torch.Tensor, p: int, stream=None):

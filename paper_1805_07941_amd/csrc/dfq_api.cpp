@@ -1052,7 +1052,168 @@ int64_t dfq_add_max_len(int q, int64_t bx, int64_t ex)
     return ((int64_t)1 << (q - 1)) / (bx + ex);
 }
 
+}  // extern "C"
+
+// ---- microscaled tensors
+
+namespace {
+
+inline bool dtype_ok(dfq_dtype t) { return t == DFQ_F32 || t == DFQ_BF16 || t == DFQ_F16; }
+inline bool elem_ok(dfq_mx_elem e) { return e == DFQ_MX4 || e == DFQ_MX8; }
+inline bool rule_ok(dfq_mx_rule r) { return r == DFQ_MX_COVER || r == DFQ_MX_FLOOR; }
+inline size_t dtype_size(dfq_dtype t) { return t == DFQ_F32 ? 4 : 2; }
+
+constexpr int kMostMxValues = 1 << 22;
+constexpr size_t kMostMxRows = 0x7fffffff;
+constexpr size_t kMostMxDistance = (size_t)1 << 40;      // bytes between rows: products with a number of rows stay in 64 bits
+
+inline size_t mx_row_bytes(dfq_mx_elem e, int K) { return (size_t)((K + 31) / 32) * (e == DFQ_MX8 ? 32 : 16); }
+
+dfq_status check_size(size_t rows, int K)
+{
+    if (K < 1) return DFQ_ESHAPE;
+    return K > kMostMxValues || rows > kMostMxRows ? DFQ_EUNSUPPORTED : DFQ_OK;
+}
+
+dfq_status check_float_rows(const void *p, size_t ld, dfq_dtype t, int K)
+{
+    if (!p || (uintptr_t)p % dtype_size(t)) return DFQ_EINVAL;
+    if (ld < (size_t)K) return DFQ_ESHAPE;
+    return ld > kMostMxDistance ? DFQ_EUNSUPPORTED : DFQ_OK;
+}
+
+dfq_status check_mx_rows(const uint8_t *codes, size_t ldc, const uint8_t *scales, size_t lds, dfq_mx_elem e, int K)
+{
+    if (!codes || !scales || (uintptr_t)codes % 16 || (uintptr_t)scales % 4) return DFQ_EINVAL;
+    if (ldc % 16 || lds % 4 || ldc < mx_row_bytes(e, K) || lds < (size_t)((K + 31) / 32)) return DFQ_ESHAPE;
+    return ldc > kMostMxDistance || lds > kMostMxDistance ? DFQ_EUNSUPPORTED : DFQ_OK;
+}
+
+inline Span float_span(const void *p, size_t ld, dfq_dtype t, size_t rows, int K)
+{
+    return {p, p && rows ? ((rows - 1) * ld + (size_t)K) * dtype_size(t) : 0};
+}
+inline Span codes_span(const uint8_t *p, size_t ldc, dfq_mx_elem e, size_t rows, int K)
+{
+    return {p, p && rows ? (rows - 1) * ldc + mx_row_bytes(e, K) : 0};
+}
+inline Span scales_span(const uint8_t *p, size_t lds, size_t rows, int K)
+{
+    return {p, p && rows ? (rows - 1) * lds + (size_t)((K + 127) / 128) * 4 : 0};
+}
+
+#define DFQ_TRY(expr)                            \
+    do {                                         \
+        const dfq_status tried_ = (expr);        \
+        if (tried_ != DFQ_OK) return tried_;     \
+    } while (0)
+
+// the operands of a product; a.M, a.N and a.K are set
+dfq_status check_linear(const LinearMxArgs &a, dfq_mx_elem ex, dfq_mx_elem ew)
+{
+    if (!elem_ok(ex) || !elem_ok(ew)) return DFQ_EINVAL;
+    if (a.N < 1) return DFQ_ESHAPE;
+    DFQ_TRY(check_size(a.M, a.K));
+    DFQ_TRY(check_mx_rows(a.x, a.ldx, a.xs, a.ldxs, ex, a.K));
+    DFQ_TRY(check_mx_rows(a.w, a.ldw, a.ws, a.ldws, ew, a.K));
+    return (uintptr_t)a.bias % 4 ? DFQ_EINVAL : DFQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+dfq_status dfq_quantize_mx(const void *x, size_t ldx, dfq_dtype dtype, size_t rows, int K, uint8_t *codes, size_t ldc, uint8_t *scales,
+                           size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, dfq_stream stream)
+{
+    if (!dtype_ok(dtype) || !elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
+    DFQ_TRY(check_size(rows, K));
+    if (!rows) return DFQ_OK;
+    DFQ_TRY(check_float_rows(x, ldx, dtype, K));
+    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, K));
+    if (!apart({float_span(x, ldx, dtype, rows, K)}, {codes_span(codes, ldc, elem, rows, K), scales_span(scales, lds, rows, K)})) return DFQ_EINVAL;
+    return from_hip(launch_quantize_mx(MxRows{x, ldx, rows, K, dtype}, MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, (hipStream_t)stream));
+}
+
+dfq_status dfq_dequantize_mx(const uint8_t *codes, size_t ldc, const uint8_t *scales, size_t lds, dfq_mx_elem elem, size_t rows, int K,
+                             void *x, size_t ldx, dfq_dtype dtype, dfq_stream stream)
+{
+    if (!dtype_ok(dtype) || !elem_ok(elem)) return DFQ_EINVAL;
+    DFQ_TRY(check_size(rows, K));
+    if (!rows) return DFQ_OK;
+    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, K));
+    DFQ_TRY(check_float_rows(x, ldx, dtype, K));
+    if (!apart({codes_span(codes, ldc, elem, rows, K), scales_span(scales, lds, rows, K)}, {float_span(x, ldx, dtype, rows, K)})) return DFQ_EINVAL;
+    return from_hip(launch_dequantize_mx(MxTensor{const_cast<uint8_t *>(codes), ldc, const_cast<uint8_t *>(scales), lds, elem}, MxRows{x, ldx, rows, K, dtype},
+                                         (hipStream_t)stream));
+}
+
+dfq_status dfq_linear_mx(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
+                         const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, void *y, size_t ldy, dfq_dtype dtype,
+                         size_t M, int N, int K, int relu, dfq_stream stream)
+{
+    LinearMxArgs a{x, x_scales, w, w_scales, ldx, ldxs, ldw, ldws, elem_x, elem_w, bias, y, ldy, dtype, {}, 0, M, N, K, relu ? 1 : 0};
+    if (!dtype_ok(dtype)) return DFQ_EINVAL;
+    if (!M) return N < 1 || K < 1 ? DFQ_ESHAPE : DFQ_OK;
+    DFQ_TRY(check_linear(a, elem_x, elem_w));
+    DFQ_TRY(check_float_rows(y, ldy, dtype, N));
+    if (!apart({codes_span(x, ldx, elem_x, M, K), scales_span(x_scales, ldxs, M, K), codes_span(w, ldw, elem_w, N, K), scales_span(w_scales, ldws, N, K),
+                {bias, (size_t)N * 4}}, {float_span(y, ldy, dtype, M, N)}))
+        return DFQ_EINVAL;
+    return from_hip(launch_linear_mx(a, (hipStream_t)stream));
+}
+
+dfq_status dfq_linear_mx_q(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
+                           const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, uint8_t *codes, size_t ldc,
+                           uint8_t *scales, size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream)
+{
+    LinearMxArgs a{x, x_scales, w, w_scales, ldx, ldxs, ldw, ldws, elem_x, elem_w, bias, nullptr, 0, DFQ_F32,
+                   MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, M, N, K, relu ? 1 : 0};
+    if (!elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
+    if (!M) return N < 1 || K < 1 ? DFQ_ESHAPE : DFQ_OK;
+    DFQ_TRY(check_linear(a, elem_x, elem_w));
+    DFQ_TRY(check_size(M, N));
+    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, N));
+    if (!apart({codes_span(x, ldx, elem_x, M, K), scales_span(x_scales, ldxs, M, K), codes_span(w, ldw, elem_w, N, K), scales_span(w_scales, ldws, N, K),
+                {bias, (size_t)N * 4}}, {codes_span(codes, ldc, elem, M, N), scales_span(scales, lds, M, N)}))
+        return DFQ_EINVAL;
+    return from_hip(launch_linear_mx(a, (hipStream_t)stream));
+}
+
+dfq_status dfq_rms_norm_mx(const void *x, size_t ldx, const void *add, size_t ldadd, void *sum, size_t ldsum, dfq_dtype dtype,
+                           const void *weight, dfq_dtype wtype, float eps, void *y, size_t ldy, uint8_t *codes, size_t ldc, uint8_t *scales,
+                           size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t rows, int K, dfq_stream stream)
+{
+    if (!dtype_ok(dtype) || !dtype_ok(wtype) || (wtype != dtype && wtype != DFQ_F32) || !elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
+    if (!(eps >= 0.0f) || std::isinf(eps)) return DFQ_EINVAL;
+    DFQ_TRY(check_size(rows, K));
+    if (!rows) return DFQ_OK;
+    if (!y && !codes) return DFQ_EINVAL;
+    DFQ_TRY(check_float_rows(x, ldx, dtype, K));
+    if (add) DFQ_TRY(check_float_rows(add, ldadd, dtype, K));
+    if (sum) DFQ_TRY(check_float_rows(sum, ldsum, dtype, K));
+    if (y) DFQ_TRY(check_float_rows(y, ldy, dtype, K));
+    if (codes) DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, K));
+    if ((uintptr_t)weight % dtype_size(wtype)) return DFQ_EINVAL;
+    // in place: a row of the sum is written where the same row was read
+    const Span xs = float_span(x, ldx, dtype, rows, K), as = float_span(add, ldadd, dtype, rows, K), ws = {weight, weight ? K * dtype_size(wtype) : 0};
+    const Span ss = float_span(sum, ldsum, dtype, rows, K), ys = float_span(y, ldy, dtype, rows, K);
+    const Span cs = codes_span(codes, ldc, elem, rows, K), es = codes ? scales_span(scales, lds, rows, K) : Span{nullptr, 0};
+    const bool on_x = sum && sum == x && (ldsum == ldx || rows == 1), on_add = sum && sum == add && (ldsum == ldadd || rows == 1);
+    if (!apart({xs, as, ws}, {ys, cs, es}) || !apart({on_x ? Span{nullptr, 0} : xs, on_add ? Span{nullptr, 0} : as, ws, ys, cs, es}, {ss})) return DFQ_EINVAL;
+    const RmsNormArgs a{MxRows{x, ldx, rows, K, dtype}, add, ldadd, sum, ldsum, weight, wtype == DFQ_F32, eps, y, ldy,
+                        MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER};
+    return from_hip(launch_rms_norm_mx(a, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
+#undef DFQ_TRY
+
+extern "C" {
+
 // ---- a pass as one call
+
 
 }  // extern "C"
 
@@ -1064,6 +1225,12 @@ inline T argument(int64_t v)
     if constexpr (std::is_pointer_v<T>) return reinterpret_cast<T>((uintptr_t)v);
     else if constexpr (std::is_same_v<T, dfq_fmt>) return dfq_fmt{8, (int32_t)v};
     else if constexpr (std::is_enum_v<T>) return (T)(int)v;
+    else if constexpr (std::is_same_v<T, float>) {
+        const uint32_t bits = (uint32_t)v;
+        float f;
+        std::memcpy(&f, &bits, sizeof f);
+        return f;
+    }
     else return (T)v;
 }
 
@@ -1095,7 +1262,8 @@ const CallEntry kCalls[] = {
     DFQ_ENTRY(dfq_conv_q_pc_maxpool), DFQ_ENTRY(dfq_quantize_conv_q_maxpool), DFQ_ENTRY(dfq_quantize_conv_q_pc_maxpool),
     DFQ_ENTRY(dfq_eltwise_q), DFQ_ENTRY(dfq_concat_q_into), DFQ_ENTRY(dfq_pool_q), DFQ_ENTRY(dfq_quantize_np), DFQ_ENTRY(dfq_dequantize_np),
     DFQ_ENTRY(dfq_np_digits), DFQ_ENTRY(dfq_conv_np), DFQ_ENTRY(dfq_conv_np_add), DFQ_ENTRY(dfq_eltwise_np), DFQ_ENTRY(dfq_pool_np),
-    DFQ_ENTRY(dfq_stem_pack_x)};
+    DFQ_ENTRY(dfq_stem_pack_x), DFQ_ENTRY(dfq_quantize_mx), DFQ_ENTRY(dfq_dequantize_mx), DFQ_ENTRY(dfq_linear_mx), DFQ_ENTRY(dfq_linear_mx_q),
+    DFQ_ENTRY(dfq_rms_norm_mx)};
 #undef DFQ_ENTRY
 constexpr int kNumCalls = (int)(sizeof(kCalls) / sizeof(kCalls[0]));
 

@@ -85,6 +85,57 @@ struct CalConcat {
     int32_t *frac_out = nullptr;
 };
 
+// Rows of floating-point values: `ld` elements apart, K of them, dtype one of dfq_dtype.
+struct MxRows {
+    const void *p;
+    size_t ld, rows;
+    int K, dtype;
+};
+
+// A microscaled tensor: rows of codes `ldc` bytes apart (both multiples of 16), rows of scale bytes `lds` apart (multiples of 4).
+struct MxTensor {
+    uint8_t *codes = nullptr;
+    size_t ldc = 0;
+    uint8_t *scales = nullptr;
+    size_t lds = 0;
+    int elem = 0;
+};
+
+struct RmsNormArgs {
+    MxRows x;
+    const void *add;        // may be null
+    size_t ldadd;
+    void *sum;              // may be null; may be x or add
+    size_t ldsum;
+    const void *weight;     // may be null
+    int weight_f32;         // float32, otherwise of x's type
+    float eps;
+    void *y;                // may be null
+    size_t ldy;
+    MxTensor q;             // codes may be null
+    int cover;
+};
+
+// y = x * w^T + bias on microscaled operands; the result in floating point (y) or converted (q.codes).
+struct LinearMxArgs {
+    const uint8_t *x, *xs, *w, *ws;
+    size_t ldx, ldxs, ldw, ldws;
+    int elem_x, elem_w;
+    const float *bias;      // may be null
+    void *y;
+    size_t ldy;
+    int dtype;
+    MxTensor q;
+    int cover;
+    size_t M;
+    int N, K, relu;
+};
+
+hipError_t launch_quantize_mx(const MxRows &x, const MxTensor &q, bool cover, hipStream_t st);
+hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t st);
+hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st);
+hipError_t launch_linear_mx(const LinearMxArgs &a, hipStream_t st);
+
 hipError_t launch_quantize(const float *x, int8_t *q, size_t n, int frac, hipStream_t st);
 hipError_t launch_quantize_i32(const float *x, int32_t *q, size_t n, int frac, hipStream_t st);
 hipError_t launch_dequantize(const int8_t *q, float *x, size_t n, int frac, hipStream_t st);

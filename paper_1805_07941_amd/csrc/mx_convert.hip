@@ -1,0 +1,208 @@
+// Conversion of float rows to microscaled ones and back, and the root-mean-square norm whose result is converted on the way out.
+// All three move bytes: a lane takes eight values (16 bytes of a 16-bit type), the four lanes of a quad a block of 32, whose largest
+// magnitude is found by two lane exchanges inside the quad.
+#include "dfq_host.hpp"
+#include "mx_device.hpp"
+#include "conv_epilogue.hpp"
+
+namespace dfq {
+
+namespace {
+
+constexpr int kBlock = 256;
+
+// every row starts on a multiple of 16 bytes
+inline int vec16(const void *p, size_t ld_bytes) { return ((uintptr_t)p | ld_bytes) % 16 == 0; }
+
+// rows * octets of one launch: 32-bit thread numbers and grids
+constexpr long long kMostOctets = 1LL << 30;
+
+template <int DT, int ELEM>
+__global__ void __launch_bounds__(kBlock) quantize_mx_kernel(const char *__restrict__ x, size_t ldx, uint8_t *__restrict__ codes, size_t ldc,
+                                                             uint8_t *__restrict__ scales, size_t lds, int K, int nb, unsigned total, FastDiv div, int vec,
+                                                             int cover)
+{
+    const unsigned t = blockIdx.x * kBlock + threadIdx.x;
+    if (t >= total) return;                          // (total is a multiple of 4: whole quads)
+    const int row = fastdiv((int)t, div), o = (int)t - row * nb * 4;
+    float v[8];
+    load_octet<DT>(v, x + (size_t)row * ldx, o, K, vec);
+    mx_store_octet<ELEM>(v, codes + (size_t)row * ldc, scales + (size_t)row * lds, o, nb, cover);
+}
+
+template <int DT, int ELEM>
+__global__ void __launch_bounds__(kBlock) dequantize_mx_kernel(const uint8_t *__restrict__ codes, size_t ldc, const uint8_t *__restrict__ scales, size_t lds,
+                                                               char *__restrict__ x, size_t ldx, int K, int no, unsigned total, FastDiv div, int vec)
+{
+    const unsigned t = blockIdx.x * kBlock + threadIdx.x;
+    if (t >= total) return;
+    const int row = fastdiv((int)t, div), o = (int)t - row * no;
+    const uint8_t *c = codes + (size_t)row * ldc;
+    uint2 w = make_uint2(0u, 0u);
+    if constexpr (ELEM == kMx4) w.x = ((const uint32_t *)c)[o];
+    else w = ((const uint2 *)c)[o];
+    float v[8];
+    mx_values<ELEM>(v, w, scales[(size_t)row * lds + (o >> 2)]);
+    store_octet<DT>(v, x + (size_t)row * ldx, o, K, vec);
+}
+
+template <int DT>
+hipError_t run_quantize(const MxRows &x, const MxTensor &q, bool cover, hipStream_t st)
+{
+    const int nb = (x.K + kMxBlock - 1) / kMxBlock;
+    const size_t most = (size_t)(kMostOctets / (nb * 4LL));
+    const int vec = vec16(x.p, x.ld * dtype_bytes<DT>());
+    for (size_t r = 0; r < x.rows; r += most) {
+        const size_t rows = x.rows - r < most ? x.rows - r : most;
+        const unsigned total = (unsigned)(rows * nb * 4);
+        const char *xp = (const char *)x.p + r * x.ld * dtype_bytes<DT>();
+        const auto kernel = q.elem == kMx8 ? quantize_mx_kernel<DT, kMx8> : quantize_mx_kernel<DT, kMx4>;
+        kernel<<<(total + kBlock - 1) / kBlock, kBlock, 0, st>>>(xp, x.ld * dtype_bytes<DT>(), q.codes + r * q.ldc, q.ldc, q.scales + r * q.lds, q.lds, x.K,
+                                                                 nb, total, make_fastdiv(nb * 4), vec, cover);
+    }
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
+{
+    const int no = (x.K + 7) / 8;
+    const size_t most = (size_t)(kMostOctets / no);
+    const int vec = vec16(x.p, x.ld * dtype_bytes<DT>());
+    for (size_t r = 0; r < x.rows; r += most) {
+        const size_t rows = x.rows - r < most ? x.rows - r : most;
+        const unsigned total = (unsigned)(rows * no);
+        char *xp = (char *)x.p + r * x.ld * dtype_bytes<DT>();
+        const auto kernel = q.elem == kMx8 ? dequantize_mx_kernel<DT, kMx8> : dequantize_mx_kernel<DT, kMx4>;
+        kernel<<<(total + kBlock - 1) / kBlock, kBlock, 0, st>>>(q.codes + r * q.ldc, q.ldc, q.scales + r * q.lds, q.lds, xp, x.ld * dtype_bytes<DT>(), x.K, no,
+                                                                 total, make_fastdiv(no), vec);
+    }
+    return hipGetLastError();
+}
+
+// ---- root-mean-square norm: s = x + add, y = s / sqrt(mean(s^2) + eps) * weight.
+// One workgroup to a row; a thread holds V octets of the sum in registers between the two passes over it (V == 0: rows too long
+// for that, the second pass reads x and add again).
+struct NormParams {
+    RmsNormArgs a;
+    int nb, vec_x, vec_add, vec_sum, vec_y, vec_w;
+};
+
+template <int DT>
+__device__ __forceinline__ void load_sum(float (&s)[8], const NormParams &p, size_t row, int o)
+{
+    constexpr int B = dtype_bytes<DT>();
+    load_octet<DT>(s, (const char *)p.a.x.p + row * p.a.x.ld * B, o, p.a.x.K, p.vec_x);
+    if (p.a.add) {
+        float t[8];
+        load_octet<DT>(t, (const char *)p.a.add + row * p.a.ldadd * B, o, p.a.x.K, p.vec_add);
+#pragma unroll
+        for (int i = 0; i < 8; i++) s[i] += t[i];
+    }
+}
+
+template <int DT, int ELEM, int T, int V>
+__global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
+{
+    constexpr int B = dtype_bytes<DT>();
+    __shared__ float part[T / 64];
+    const size_t row = blockIdx.x;
+    const int K = p.a.x.K, octets = p.nb * 4;
+    float s[V > 0 ? V : 1][8];
+    float sq = 0.0f;
+    auto visit = [&](float (&v)[8], int o) __attribute__((always_inline)) {
+        load_sum<DT>(v, p, row, o);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sq += v[i] * v[i];
+    };
+    if constexpr (V > 0) {
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const int o = j * T + threadIdx.x;
+            if (o < octets) visit(s[j], o);
+        }
+    } else {
+        for (int o = threadIdx.x; o < octets; o += T) visit(s[0], o);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) sq += __shfl_xor(sq, off, kWave);
+    if constexpr (T > 64) {
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sq;
+        __syncthreads();
+        sq = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T / 64; i++) sq += part[i];
+    }
+    const float r = 1.0f / sqrtf(sq / (float)K + p.a.eps);
+
+    auto finish = [&](float (&v)[8], int o) __attribute__((always_inline)) {
+        if (p.a.sum) store_octet<DT>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K, p.vec_sum);
+        float w[8];
+        if (!p.a.weight) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) w[i] = 1.0f;
+        } else if (p.a.weight_f32) {
+            load_octet<kF32>(w, p.a.weight, o, K, p.vec_w);
+        } else {
+            load_octet<DT>(w, p.a.weight, o, K, p.vec_w);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * r * w[i] : 0.0f;      // (zeros behind K whatever r is)
+        if (p.a.y) store_octet<DT>(v, (char *)p.a.y + row * p.a.ldy * B, o, K, p.vec_y);
+        if (p.a.q.codes) mx_store_octet<ELEM>(v, p.a.q.codes + row * p.a.q.ldc, p.a.q.scales + row * p.a.q.lds, o, p.nb, p.a.cover);
+    };
+    if constexpr (V > 0) {
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const int o = j * T + threadIdx.x;
+            if (o < octets) finish(s[j], o);
+        }
+    } else {
+        for (int o = threadIdx.x; o < octets; o += T) {
+            load_sum<DT>(s[0], p, row, o);
+            finish(s[0], o);
+        }
+    }
+}
+
+template <int DT, int ELEM>
+hipError_t run_norm(const NormParams &p, hipStream_t st)
+{
+    const int octets = p.nb * 4;
+    const unsigned rows = (unsigned)p.a.x.rows;
+    if (octets <= 64) rms_norm_mx_kernel<DT, ELEM, 64, 1><<<rows, 64, 0, st>>>(p);
+    else if (octets <= 256) rms_norm_mx_kernel<DT, ELEM, 256, 1><<<rows, 256, 0, st>>>(p);
+    else if (octets <= 1024) rms_norm_mx_kernel<DT, ELEM, 256, 4><<<rows, 256, 0, st>>>(p);
+    else if (octets <= 4096) rms_norm_mx_kernel<DT, ELEM, 1024, 4><<<rows, 1024, 0, st>>>(p);
+    else rms_norm_mx_kernel<DT, ELEM, 1024, 0><<<rows, 1024, 0, st>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize_mx(const MxRows &x, const MxTensor &q, bool cover, hipStream_t st)
+{
+    return x.dtype == kF32 ? run_quantize<kF32>(x, q, cover, st) : x.dtype == kBF16 ? run_quantize<kBF16>(x, q, cover, st) : run_quantize<kF16>(x, q, cover, st);
+}
+
+hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t st)
+{
+    return x.dtype == kF32 ? run_dequantize<kF32>(q, x, st) : x.dtype == kBF16 ? run_dequantize<kBF16>(q, x, st) : run_dequantize<kF16>(q, x, st);
+}
+
+hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st)
+{
+    const int B = a.x.dtype == kF32 ? 4 : 2;
+    NormParams p{a, (a.x.K + kMxBlock - 1) / kMxBlock};
+    p.vec_x = vec16(a.x.p, a.x.ld * B);
+    p.vec_add = vec16(a.add, a.ldadd * B);
+    p.vec_sum = vec16(a.sum, a.ldsum * B);
+    p.vec_y = vec16(a.y, a.ldy * B);
+    p.vec_w = vec16(a.weight, 0);
+    const bool mx8 = a.q.elem == kMx8;
+    if (a.x.dtype == kF32) return mx8 ? run_norm<kF32, kMx8>(p, st) : run_norm<kF32, kMx4>(p, st);
+    if (a.x.dtype == kBF16) return mx8 ? run_norm<kBF16, kMx8>(p, st) : run_norm<kBF16, kMx4>(p, st);
+    return mx8 ? run_norm<kF16, kMx8>(p, st) : run_norm<kF16, kMx4>(p, st);
+}
+
+}  // namespace dfq
