@@ -338,110 +338,145 @@ class MxTensor(NamedTuple):
 
     @classmethod
     def empty(cls, rows: int, k: int, elem: int, device="cuda") -> "MxTensor":
-        nb = (k + 31) // 32
-        return cls(torch.empty((rows, nb * (32 if elem == MX8 else 16)), dtype=torch.uint8, device=device),
-                   torch.empty((rows, (nb + 3) // 4 * 4), dtype=torch.uint8, device=device), elem, k)
+        nb = (k + 31) >> 5
+        return cls(torch.empty((rows, nb << 5 if elem == MX8 else nb << 4), dtype=torch.uint8, device=device),
+                   torch.empty((rows, nb + 3 & -4), dtype=torch.uint8, device=device), elem, k)
 
 
+# (What these check is read once: a call on one token is bound by the host.)
 def _here(t: torch.Tensor, name: str):
     """A launch goes to the current device."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    at = t.get_device()
+    if at < 0 or at != _current_device():
         raise ValueError(f"{name}: expected a tensor on the current CUDA device")
 
 
 def _rows(t: torch.Tensor, name: str, dtype=None):
-    """[rows, k] with whole rows, or a contiguous tensor of more dimensions as its rows."""
-    _here(t, name)
+    """(address, row distance, rows, k) of [rows, k] with whole rows, or of a contiguous tensor of more dimensions as its rows."""
+    at = t.get_device()
+    if at < 0 or at != _current_device():
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device")
     if (t.dtype is not dtype) if dtype is not None else t.dtype not in MX_DTYPES:
         raise TypeError(f"{name}: expected {dtype or 'float32, bfloat16 or float16'}")
-    if t.dim() != 2:
-        if t.dim() == 0 or not t.is_contiguous():
-            raise ValueError(f"{name}: expected [rows, k] or a contiguous tensor")
-        t = t.view(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the values of a row have to be next to each other")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError(f"{name}: rows overlap")
-    return t
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    shape = t.shape
+    if len(shape) == 2:
+        rows, k = shape
+        ld, step = t.stride()
+        if k > 1 and step != 1:
+            raise ValueError(f"{name}: the values of a row have to be next to each other")
+        if rows <= 1:
+            ld = k
+        elif ld < k:
+            raise ValueError(f"{name}: rows overlap")
+        return t.data_ptr(), ld, rows, k
+    if not shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected [rows, k] or a contiguous tensor")
+    k = shape[-1]
+    return t.data_ptr(), k, t.numel() // k if k else 0, k
 
 
 def _mx(q: MxTensor, name: str, rows: Optional[int] = None, k: Optional[int] = None):
-    """Checks a microscaled tensor; returns (codes, their row distance, scales, their row distance)."""
-    c, s = q.codes, q.scales
-    for t, what in ((c, "codes"), (s, "scales")):
-        _rows(t, f"{name}.{what}", torch.uint8)
-        if t.dim() != 2:
-            raise ValueError(f"{name}.{what}: expected [rows, bytes]")
-    if q.elem not in (MX4, MX8) or q.k < 1:
+    """Checks a microscaled tensor; returns (codes, their row distance, scales, their row distance) and its number of rows."""
+    codes, scales, elem, n = q
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError(f"{name}: expected [rows, bytes]")
+    c, ldc, have, width = _rows(codes, name, torch.uint8)
+    s, lds, srows, swidth = _rows(scales, name, torch.uint8)
+    if elem not in (MX4, MX8) or n < 1:
         raise ValueError(f"{name}: no such element, or no values")
-    nb = (q.k + 31) // 32
-    if c.shape[0] != s.shape[0] or c.shape[1] < nb * (32 if q.elem == MX8 else 16) or s.shape[1] < (nb + 3) // 4 * 4:
-        raise ValueError(f"{name}: codes and scales do not hold rows of {q.k} values")
-    if (rows is not None and c.shape[0] != rows) or (k is not None and q.k != k):
-        raise ValueError(f"{name}: expected {rows if rows is not None else c.shape[0]} rows of {k if k is not None else q.k} values")
-    return c.data_ptr(), _ld(c), s.data_ptr(), _ld(s)
+    nb = (n + 31) >> 5
+    if have != srows or width < (nb << 5 if elem == MX8 else nb << 4) or swidth < nb + 3 & -4:
+        raise ValueError(f"{name}: codes and scales do not hold rows of {n} values")
+    if (rows is not None and have != rows) or (k is not None and n != k):
+        raise ValueError(f"{name}: expected {have if rows is None else rows} rows of {n if k is None else k} values")
+    return (c, ldc, s, lds), have
 
 
 def _allocating_on(stream):
     """New tensors belong to the stream that writes them."""
-    if stream is None:
-        return nullcontext()
     return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+
+
+def _new(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _allocating_on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _new_mx(rows: int, k: int, elem: int, device, stream):
+    """A fresh microscaled tensor, and what _mx gives for it."""
+    if stream is None:
+        q = MxTensor.empty(rows, k, elem, device)
+    else:
+        with _allocating_on(stream):
+            q = MxTensor.empty(rows, k, elem, device)
+    nb = (k + 31) >> 5
+    return q, (q.codes.data_ptr(), nb << 5 if elem == MX8 else nb << 4, q.scales.data_ptr(), nb + 3 & -4)
+
+
+def _out_mx(out: MxTensor, rows: int, k: int, elem: int):
+    if out.elem != elem:
+        raise ValueError("out: holds other elements")
+    return out, _mx(out, "out", rows, k)[0]
+
+
+def _out_rows(out: torch.Tensor, name: str, dtype: torch.dtype, rows: int, k: int):
+    at, ld, r, n = _rows(out, name, dtype)
+    if r != rows or n != k:
+        raise ValueError(f"{name}: expected {rows} rows of {k} values")
+    return at, ld
+
+
+def _dtype_code(dtype: torch.dtype) -> int:
+    code = MX_DTYPES.get(dtype)
+    if code is None:
+        raise TypeError("dtype: expected float32, bfloat16 or float16")
+    return code
 
 
 def quantize_mx(x: torch.Tensor, elem: int = MX8, rule: int = MX_COVER, out: Optional[MxTensor] = None, stream=None) -> MxTensor:
     """float32, bfloat16 or float16 rows -> microscaled ones; the rows of a tensor of more dimensions are its last one's."""
-    x = _rows(x, "x")
-    rows, k = x.shape
-    if out is None:
-        with _allocating_on(stream):
-            out = MxTensor.empty(rows, k, elem, x.device)
-    elif out.elem != elem:
-        raise ValueError("out: holds other elements")
-    c, ldc, s, lds = _mx(out, "out", rows, k)
-    _check(lib().dfq_quantize_mx(x.data_ptr(), _ld(x), MX_DTYPES[x.dtype], rows, k, c, ldc, s, lds, int(elem), int(rule), _stream(stream)), "dfq_quantize_mx")
+    at, ld, rows, k = _rows(x, "x")
+    out, q = _new_mx(rows, k, elem, x.device, stream) if out is None else _out_mx(out, rows, k, elem)
+    _check(lib().dfq_quantize_mx(at, ld, MX_DTYPES[x.dtype], rows, k, *q, elem, rule, _stream(stream)), "dfq_quantize_mx")
     return out
 
 
 def dequantize_mx(q: MxTensor, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values of a microscaled tensor, [rows, k]."""
-    c, ldc, s, lds = _mx(q, "q")
-    rows = q.codes.shape[0]
+    held, rows = _mx(q, "q")
+    code, k = _dtype_code(dtype), q.k
     if out is None:
-        with _allocating_on(stream):
-            out = torch.empty((rows, q.k), dtype=dtype, device=q.codes.device)
-    x = _rows(out, "out", dtype)
-    if dtype not in MX_DTYPES or x.shape != (rows, q.k):
-        raise ValueError(f"out: expected [{rows}, {q.k}] of float32, bfloat16 or float16")
-    _check(lib().dfq_dequantize_mx(c, ldc, s, lds, q.elem, rows, q.k, x.data_ptr(), _ld(x), MX_DTYPES[dtype], _stream(stream)), "dfq_dequantize_mx")
+        out = _new((rows, k), dtype, q.codes.device, stream)
+        at, ld = out.data_ptr(), k
+    else:
+        at, ld = _out_rows(out, "out", dtype, rows, k)
+    _check(lib().dfq_dequantize_mx(*held, q.elem, rows, k, at, ld, code, _stream(stream)), "dfq_dequantize_mx")
     return out
 
 
 def _linear_operands(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor]):
-    xa, wa = _mx(x, "x"), _mx(w, "w", None, x.k)
-    n = w.codes.shape[0]
-    if bias is not None:
-        _here(bias, "bias")
-        if bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous():
-            raise ValueError(f"bias: expected {n} contiguous float32 values")
-    return x.codes.shape[0], n, (*xa, x.elem, *wa, w.elem, _ptr(bias))
+    (xa, m), (wa, n) = _mx(x, "x"), _mx(w, "w", None, x.k)
+    if bias is None:
+        return m, n, (*xa, x.elem, *wa, w.elem, None)
+    _here(bias, "bias")
+    if bias.dtype is not torch.float32 or bias.shape != (n,) or not bias.is_contiguous():
+        raise ValueError(f"bias: expected {n} contiguous float32 values")
+    return m, n, (*xa, x.elem, *wa, w.elem, bias.data_ptr())
 
 
 def linear_mx(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, relu: bool = False, dtype: torch.dtype = torch.bfloat16,
               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """x [m, k] times w [n, k] transposed, plus bias [n] float32, with relu max(., 0): [m, n] of dtype."""
     m, n, operands = _linear_operands(x, w, bias)
+    code = _dtype_code(dtype)
     if out is None:
-        with _allocating_on(stream):
-            out = torch.empty((m, n), dtype=dtype, device=x.codes.device)
-    y = _rows(out, "out", dtype)
-    if dtype not in MX_DTYPES or y.shape != (m, n):
-        raise ValueError(f"out: expected [{m}, {n}] of float32, bfloat16 or float16")
-    _check(lib().dfq_linear_mx(*operands, y.data_ptr(), _ld(y), MX_DTYPES[dtype], m, n, x.k, int(bool(relu)), _stream(stream)), "dfq_linear_mx")
+        out = _new((m, n), dtype, x.codes.device, stream)
+        at, ld = out.data_ptr(), n
+    else:
+        at, ld = _out_rows(out, "out", dtype, m, n)
+    _check(lib().dfq_linear_mx(*operands, at, ld, code, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx")
     return out
 
 
@@ -449,12 +484,8 @@ def linear_mx_q(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, e
                 out: Optional[MxTensor] = None, stream=None) -> MxTensor:
     """The same with the result converted for the next product."""
     m, n, operands = _linear_operands(x, w, bias)
-    if out is None:
-        with _allocating_on(stream):
-            out = MxTensor.empty(m, n, elem, x.codes.device)
-    elif out.elem != elem:
-        raise ValueError("out: holds other elements")
-    _check(lib().dfq_linear_mx_q(*operands, *_mx(out, "out", m, n), int(elem), int(rule), m, n, x.k, int(bool(relu)), _stream(stream)), "dfq_linear_mx_q")
+    out, q = _new_mx(m, n, elem, x.codes.device, stream) if out is None else _out_mx(out, m, n, elem)
+    _check(lib().dfq_linear_mx_q(*operands, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx_q")
     return out
 
 
@@ -463,30 +494,31 @@ def rms_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: flo
                 sum_out: Optional[torch.Tensor] = None, stream=None):
     """Root-mean-square norm of the rows of x + add, times weight [k] (of x's type or float32), in float32.  Returns (the result converted, or
     None for elem=None; the result in x's type with want_y, else None; x + add in x's type, None without add).  sum_out may be x or add."""
-    xr = _rows(x, "x")
-    rows, k = xr.shape
+    at, ld, rows, k = _rows(x, "x")
     dt = x.dtype
-    ar = None if add is None else _rows(add, "add", dt)
-    if ar is not None and ar.shape != xr.shape:
-        raise ValueError("x and add do not match")
+    code = wcode = MX_DTYPES[dt]
+    a, lda, wp = None, 0, None
+    if add is not None:
+        a, lda = _out_rows(add, "add", dt, rows, k)
     if weight is not None:
         _here(weight, "weight")
         if weight.dtype not in (dt, torch.float32) or weight.shape != (k,) or not weight.is_contiguous():
             raise ValueError(f"weight: expected {k} contiguous values of x's type or float32")
-    with _allocating_on(stream):
-        if elem is not None and out is None:
-            out = MxTensor.empty(rows, k, elem, x.device)
-        y = torch.empty(x.shape, dtype=dt, device=x.device) if want_y else None
-        total = sum_out if sum_out is not None else torch.empty(x.shape, dtype=dt, device=x.device) if add is not None else None
-    if out is not None and out.elem != elem:
-        raise ValueError("out: holds other elements")
-    sr = None if total is None else _rows(total, "sum_out", dt)
-    if sr is not None and sr.shape != xr.shape:
-        raise ValueError("sum_out: expected the rows of x")
-    q = (None, 0, None, 0) if out is None else _mx(out, "out", rows, k)
-    _check(lib().dfq_rms_norm_mx(xr.data_ptr(), _ld(xr), _ptr(ar), 0 if ar is None else _ld(ar), _ptr(sr), 0 if sr is None else _ld(sr), MX_DTYPES[dt],
-                                 _ptr(weight), MX_DTYPES[dt if weight is None else weight.dtype], float(eps), _ptr(y), k, *q,
-                                 MX8 if elem is None else int(elem), int(rule), rows, k, _stream(stream)), "dfq_rms_norm_mx")
+        wp, wcode = weight.data_ptr(), MX_DTYPES[weight.dtype]
+    q = (None, 0, None, 0)
+    if elem is not None:
+        out, q = _new_mx(rows, k, elem, x.device, stream) if out is None else _out_mx(out, rows, k, elem)
+    elif out is not None:
+        raise ValueError("out: nothing is converted with elem=None")
+    y = _new(x.shape, dt, x.device, stream) if want_y else None
+    total, sp, ldsum = sum_out, None, k
+    if total is not None:
+        sp, ldsum = _out_rows(total, "sum_out", dt, rows, k)
+    elif add is not None:
+        total = _new(x.shape, dt, x.device, stream)
+        sp = total.data_ptr()
+    _check(lib().dfq_rms_norm_mx(at, ld, a, lda, sp, ldsum, code, wp, wcode, eps, _ptr(y), k, *q, MX8 if elem is None else elem, rule, rows, k,
+                                 _stream(stream)), "dfq_rms_norm_mx")
     return out, y, total
 
 

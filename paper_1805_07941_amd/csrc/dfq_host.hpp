@@ -135,6 +135,9 @@ hipError_t launch_quantize_mx(const MxRows &x, const MxTensor &q, bool cover, hi
 hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t st);
 hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st);
 hipError_t launch_linear_mx(const LinearMxArgs &a, hipStream_t st);
+hipError_t launch_linear_mx_small(const LinearMxArgs &a, hipStream_t st);
+bool linear_mx_tiles_supports(const LinearMxArgs &a);
+hipError_t launch_linear_mx_tiles(const LinearMxArgs &a, hipStream_t st);
 
 hipError_t launch_quantize(const float *x, int8_t *q, size_t n, int frac, hipStream_t st);
 hipError_t launch_quantize_i32(const float *x, int32_t *q, size_t n, int frac, hipStream_t st);

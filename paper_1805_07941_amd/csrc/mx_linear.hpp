@@ -19,9 +19,6 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-// results that are converted, beside the types of dfq_dtype
-constexpr int kToMx4 = 4, kToMx8 = 5;
-
 __host__ inline void advance_tokens(LinearMxArgs &a, size_t m)
 {
     a.x += m * a.ldx;
@@ -108,7 +105,6 @@ __device__ __forceinline__ v4f multiply16(const Frag16<EW, EXACT> &w, const Frag
 }
 
 // Octet o (features 8o ..) of token m: bias, ReLU, rounding and the store.  Converted results: the four lanes of a quad hold a block.
-template <int DT>
 __device__ __forceinline__ void finish_octet(float (&v)[8], const LinearMxArgs &a, size_t m, int o)
 {
     const int n = o * 8;
@@ -117,14 +113,18 @@ __device__ __forceinline__ void finish_octet(float (&v)[8], const LinearMxArgs &
         if (a.bias && n + j < a.N) v[j] += a.bias[n + j];
         if (a.relu) v[j] = relu_f32(v[j]);
     }
-    if constexpr (DT == kToMx4 || DT == kToMx8) {
+    if (a.q.codes) {
         const int nb = (a.N + kMxBlock - 1) / kMxBlock;
         if (o >= nb * 4) return;                                  // (whole quads)
 #pragma unroll
         for (int j = 0; j < 8; j++) v[j] = n + j < a.N ? v[j] : 0.0f;
-        mx_store_octet<DT == kToMx8 ? kMx8 : kMx4>(v, a.q.codes + m * a.q.ldc, a.q.scales + m * a.q.lds, o, nb, a.cover);
+        uint8_t *codes = a.q.codes + m * a.q.ldc, *scales = a.q.scales + m * a.q.lds;
+        if (a.q.elem == kMx8) mx_store_octet<kMx8>(v, codes, scales, o, nb, a.cover);
+        else mx_store_octet<kMx4>(v, codes, scales, o, nb, a.cover);
     } else if (n < a.N) {
-        store_octet<DT>(v, (char *)a.y + m * a.ldy * dtype_bytes<DT>(), o, a.N, ((uintptr_t)a.y | a.ldy * dtype_bytes<DT>()) % 16 == 0);
+        if (a.dtype == kF32) store_octet<kF32>(v, (char *)a.y + m * a.ldy * 4, o, a.N, ((uintptr_t)a.y | a.ldy * 4) % 16 == 0);
+        else if (a.dtype == kBF16) store_octet<kBF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, ((uintptr_t)a.y | a.ldy * 2) % 16 == 0);
+        else store_octet<kF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, ((uintptr_t)a.y | a.ldy * 2) % 16 == 0);
     }
 }
 

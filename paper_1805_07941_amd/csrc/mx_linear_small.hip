@@ -14,7 +14,7 @@ namespace {
 
 // EXACT: the elements times their scales as bfloat16 (they fit its significand) on the bfloat16 matrix instructions, whose products
 // and sums keep float32's accuracy; see launch_linear_mx.
-template <int EX, int EW, bool EXACT, int DT, int FT, int TT, int NW>
+template <int EX, int EW, bool EXACT, int FT, int TT, int NW>
 __global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a)
 {
     constexpr int F = FT * 16, T = TT * 16;
@@ -89,11 +89,11 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a
                 v[4 + j] += p[1][j];
             }
         }
-        if (m < a.M) finish_octet<DT>(v, a, m, n0 / 8 + o);
+        if (m < a.M) finish_octet(v, a, m, n0 / 8 + o);
     }
 }
 
-template <int EX, int EW, bool EXACT, int DT>
+template <int EX, int EW, bool EXACT>
 hipError_t run(const LinearMxArgs &a, hipStream_t st)
 {
     constexpr int FT = 2, TT = 1, NW = 4;
@@ -103,7 +103,7 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
         advance_tokens(b, m);
         b.M = a.M - m < most * TT * 16 ? a.M - m : most * TT * 16;
         const dim3 grid((unsigned)((a.N + FT * 16 - 1) / (FT * 16)), (unsigned)((b.M + TT * 16 - 1) / (TT * 16)));
-        linear_mx_small_kernel<EX, EW, EXACT, DT, FT, TT, NW><<<grid, NW * 64, 0, st>>>(b);
+        linear_mx_small_kernel<EX, EW, EXACT, FT, TT, NW><<<grid, NW * 64, 0, st>>>(b);
     }
     return hipGetLastError();
 }
@@ -111,17 +111,23 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
 template <int EX, int EW>
 hipError_t by_output(const LinearMxArgs &a, hipStream_t st)
 {
-    if (a.q.codes) return a.q.elem == kMx8 ? run<EX, EW, false, kToMx8>(a, st) : run<EX, EW, false, kToMx4>(a, st);
-    if (a.dtype == kF32) return run<EX, EW, EX == kMx8 || EW == kMx8, kF32>(a, st);
-    return a.dtype == kBF16 ? run<EX, EW, false, kBF16>(a, st) : run<EX, EW, false, kF16>(a, st);
+    if constexpr (EX == kMx8 || EW == kMx8)
+        if (!a.q.codes && a.dtype == kF32) return run<EX, EW, true>(a, st);
+    return run<EX, EW, false>(a, st);
 }
 
 }  // namespace
 
-hipError_t launch_linear_mx(const LinearMxArgs &a, hipStream_t st)
+hipError_t launch_linear_mx_small(const LinearMxArgs &a, hipStream_t st)
 {
     if (a.elem_x == kMx4) return a.elem_w == kMx4 ? by_output<kMx4, kMx4>(a, st) : by_output<kMx4, kMx8>(a, st);
     return a.elem_w == kMx4 ? by_output<kMx8, kMx4>(a, st) : by_output<kMx8, kMx8>(a, st);
+}
+
+hipError_t launch_linear_mx(const LinearMxArgs &a, hipStream_t st)
+{
+    if (a.M > 128 && linear_mx_tiles_supports(a)) return launch_linear_mx_tiles(a, st);
+    return launch_linear_mx_small(a, st);
 }
 
 }  // namespace dfq

@@ -1,0 +1,344 @@
+// The inner product on microscaled operands for results that fill the chip: tiles of tokens x features from operands staged in LDS.
+//
+// acc[n][m] = sum_k w[n][k] * x[m][k]: features are the rows of the matrix instruction's first operand and tokens the columns of its
+// second; feature rows lie in LDS in an order that leaves 16 consecutive features of one token in each lane.  A workgroup walks the
+// reduction axis in steps of 128 bytes of an operand row (256 values of 4 bits, 128 where an operand has 8) through a ring of LDS
+// stages that direct global -> LDS loads fill, one barrier to a step.  A wavefront waits for its own loads of the step it is about to
+// read only, and reads the operands of the instruction after next while the matrix pipe is busy with this one.
+//
+// Scales come in chunks of 16 bytes of a row (512 values): a row's four bytes of one step would cost as many cache lines as its 128
+// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c; three buffers, because loads run NST steps ahead of
+// the reads.  What lies behind a row's last block is masked twice: codes by an offset past the buffer (zeros arrive), scales by a
+// comparison when they are read, so that neither the next row's bytes nor padding count.
+#include "conv_ring.hpp"
+#include "mx_linear.hpp"
+
+namespace dfq {
+
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+struct TileParams {
+    LinearMxArgs a;
+    int nb;                  // blocks of a row
+    int steps;
+    int tiles_m, tiles_n;
+};
+
+// 4 bytes per lane straight into LDS: lane l's land at lds_base + 4 * l
+__device__ __forceinline__ void load_word_to_lds(unsigned voffset, v4i rsrc, unsigned lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voffset), "s"(rsrc), "s"(lds_base) : "memory", "m0");
+}
+
+template <int ELEM, int KS>
+struct Operand {
+    static constexpr int kRow = KS * (ELEM == kMx8 ? 8 : 4) / 8;      // bytes of a row in a stage
+    static constexpr int kPieces16 = kRow / 16;
+    static_assert(kRow == 64 || kRow == 128, "LDS rows");
+    // physical place of a row's logical piece: 16 consecutive rows put one piece on all banks
+    __device__ static __forceinline__ int place(int row, int piece) { return kRow == 128 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3); }
+};
+
+// One lane's operands of a 32-row group for 64 values: what v_mfma_scale_f32_32x32x64_f8f6f4 wants (with h = lane / 32: of 4-bit
+// elements block h, of 8-bit ones bytes 16h.. of both blocks), and block h's scale byte.  EXACT: bytes 16h.. (4 bits: 8h..) of both
+// blocks, and both scales.
+template <int ELEM, bool EXACT>
+struct Frag32 {
+    v4i lo, hi;
+    unsigned scale, scale1;
+};
+
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int NST>
+__global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_kernel(TileParams prm)
+{
+    constexpr int NW = WM * WN;
+    constexpr int KS = EX == kMx4 && EW == kMx4 ? 256 : 128;
+    constexpr int KK = KS / 64;                                        // matrix instructions along a step
+    using OX = Operand<EX, KS>;
+    using OW = Operand<EW, KS>;
+    constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int XL = BM * OX::kRow / 1024 / NW, WL = BN * OW::kRow / 1024 / NW;     // code loads of a wavefront in a step
+    constexpr int SPC = 512 / KS;                                      // steps of a chunk of scales
+    constexpr int SL = (BM + BN) / 16 / SPC / NW;                      // scale loads of a wavefront in a step
+    static_assert(XL * NW * 1024 == BM * OX::kRow && WL * NW * 1024 == BN * OW::kRow && SL * SPC * NW * 16 == BM + BN, "whole loads");
+    constexpr int LPS = XL + WL + SL;
+    static_assert(NST >= 2 && NST <= SPC + 1, "three chunks of scales");
+    static_assert(NST * LPS < 64 && SPC * SL + NST * LPS < 64, "outstanding loads fit the counter");
+    constexpr int kStage = BM * OX::kRow + BN * OW::kRow;
+    constexpr int kChunk = (BM + BN) * 16;
+
+    extern __shared__ char lds[];                                      // NST stages, then three chunks of scales
+    const LinearMxArgs &a = prm.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+
+    // ---- this workgroup's tile.  Workgroups are dealt round-robin to the 8 XCDs: each gets a contiguous run of tiles, in groups of
+    // four token tiles that share the feature tiles they pass
+    int t = blockIdx.x;
+    {
+        const int G = gridDim.x, per = G / 8, rem = G % 8, xcd = t % 8, idx = t / 8;
+        t = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + idx;
+    }
+    constexpr int kGroup = 4;
+    const int group = t / (kGroup * prm.tiles_n), in = t - group * kGroup * prm.tiles_n;
+    const int rows = min(kGroup, prm.tiles_m - group * kGroup);
+    const size_t m0 = (size_t)(group * kGroup + in % rows) * BM;
+    const int n0 = in / rows * BN;
+
+    const int mrows = (int)(a.M - m0 < BM ? a.M - m0 : BM), nrows = min(a.N - n0, BN);
+    const unsigned xrow = (unsigned)(prm.nb * mx_block_bytes(EX)), wrow = (unsigned)(prm.nb * mx_block_bytes(EW));
+    const unsigned srow = (unsigned)(prm.nb + 3) & ~3u;
+    const unsigned ldx = (unsigned)a.ldx, ldw = (unsigned)a.ldw, ldxs = (unsigned)a.ldxs, ldws = (unsigned)a.ldws;
+    const v4i xr = make_rsrc(a.x + m0 * a.ldx, (unsigned)(mrows - 1) * ldx + xrow);
+    const v4i wr = make_rsrc(a.w + (size_t)n0 * a.ldw, (unsigned)(nrows - 1) * ldw + wrow);
+    const v4i xsr = make_rsrc(a.xs + m0 * a.ldxs, (unsigned)(mrows - 1) * ldxs + srow);
+    const v4i wsr = make_rsrc(a.ws + (size_t)n0 * a.ldws, (unsigned)(nrows - 1) * ldws + srow);
+    const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char *)(char *)&lds[0];
+
+    // feature of LDS row r of the weights (within the tile): row 8g + 4h + e of a group of 32 holds feature 16h + 4g + e
+    auto feature_of = [](int r) { return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r & 31) >> 3) + (r & 3); };
+
+    // ---- producer: a wavefront-wide load fills 1024 bytes of a stage, rows lane / pieces of it; the lane's logical piece is the same
+    // in every load (the number of wavefronts is even)
+    constexpr int XR = 64 / OX::kPieces16, WR = 64 / OW::kPieces16;    // rows of a load
+    const int xp = OX::place(XR * wave + lane / OX::kPieces16, lane % OX::kPieces16) * 16;
+    const int wp = OW::place(WR * wave + lane / OW::kPieces16, lane % OW::kPieces16) * 16;
+    unsigned xoff[XL], woff[WL], soff[SPC * SL];
+#pragma unroll
+    for (int j = 0; j < XL; j++) {
+        const int r = XR * (wave + NW * j) + lane / OX::kPieces16;
+        xoff[j] = r < mrows ? (unsigned)r * ldx + xp : kOutOfRange;
+    }
+#pragma unroll
+    for (int j = 0; j < WL; j++) {
+        const int n = feature_of(WR * (wave + NW * j) + lane / OW::kPieces16);
+        woff[j] = n < nrows ? (unsigned)n * ldw + wp : kOutOfRange;
+    }
+    // scales: a load fills 16 rows of a chunk, rows 0 .. BM-1 the tokens', then the features' in their LDS order
+    static_assert(BM % 16 == 0, "a load of scales has rows of one operand");
+#pragma unroll
+    for (int j = 0; j < SPC * SL; j++) {
+        const int first = 16 * (wave + NW * j), r = first + lane / 4;
+        if (first < BM) {
+            soff[j] = r < mrows ? (unsigned)r * ldxs + (lane & 3) * 4 : kOutOfRange;
+        } else {
+            const int n = feature_of(r - BM);
+            soff[j] = n < nrows ? (unsigned)n * ldws + (lane & 3) * 4 : kOutOfRange;
+        }
+    }
+    auto issue_scales = [&](unsigned off, int j, int chunk) __attribute__((always_inline)) {
+        const int first = 16 * (wave + NW * j);
+        const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds_base + NST * kStage + (unsigned)(chunk % 3) * kChunk + (unsigned)first * 16));
+        const bool x = first < BM;
+        const v4i r = {x ? xsr.x : wsr.x, x ? xsr.y : wsr.y, x ? xsr.z : wsr.z, wsr.w};
+        load_word_to_lds(off + (unsigned)chunk * 16, r, dst);
+    };
+    // (without a branch: the compiler would sink the matrix instructions in front of one behind it)
+    auto issue = [&](int step, int stage) __attribute__((always_inline)) {
+        const unsigned base = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds_base + (unsigned)stage * kStage + (unsigned)wave * 1024u));
+        const unsigned kx = (unsigned)step * OX::kRow, kw = (unsigned)step * OW::kRow;
+        const unsigned badx = kx + xp < xrow ? 0u : kOutOfRange, badw = kw + wp < wrow ? 0u : kOutOfRange;
+#pragma unroll
+        for (int j = 0; j < XL; j++) load_piece_to_lds((xoff[j] + kx) | badx, xr, base + (unsigned)j * (NW * 1024u));
+#pragma unroll
+        for (int j = 0; j < WL; j++) load_piece_to_lds((woff[j] + kw) | badw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
+        const int part = step % SPC, chunk = step / SPC + 1;
+#pragma unroll
+        for (int j = 0; j < SL; j++) {
+            unsigned off = soff[j];
+#pragma unroll
+            for (int p = 1; p < SPC; p++) off = part == p ? soff[p * SL + j] : off;
+            issue_scales(off, part * SL + j, chunk);
+        }
+    };
+
+    // ---- consumer
+    const int wm0 = wave % WM * (BM / WM), wn0 = wave / WM * (BN / WN);
+    struct Set {
+        Frag32<EW, EXACT> w[TN];
+        Frag32<EX, EXACT> x[TM];
+    };
+    Set f0, f1;
+    // Addresses: a lane's row and the key of its pieces are the same in every group of 32 rows; the groups differ by constants.
+    const unsigned xlane = (unsigned)(wm0 + l32) * OX::kRow, wlane = (unsigned)(BM * OX::kRow + (wn0 + l32) * OW::kRow);
+    const unsigned xkey = OX::place(l32, 0) * 16, wkey = OW::place(l32, 0) * 16;
+    const unsigned xslane = (unsigned)(NST * kStage + (wm0 + l32) * 16), wslane = (unsigned)(NST * kStage + (BM + wn0 + l32) * 16);
+    auto read_rows = [&](auto &f, auto op, unsigned at, unsigned key, unsigned scale_at, int kk, unsigned b0, unsigned b1) __attribute__((always_inline)) {
+        constexpr bool wide = decltype(op)::kRow * 8 / KS == 8;
+        if constexpr (wide) {
+            f.lo = *(const v4i *)(lds + at + (((4 * kk + h) * 16) ^ key));
+            f.hi = *(const v4i *)(lds + at + (((4 * kk + 2 + h) * 16) ^ key));
+        } else if constexpr (EXACT) {
+            typedef int v2i __attribute__((ext_vector_type(2)));
+            const v2i p0 = *(const v2i *)(lds + at + ((2 * kk * 16) ^ key) + 8 * h), p1 = *(const v2i *)(lds + at + (((2 * kk + 1) * 16) ^ key) + 8 * h);
+            f.lo = v4i{p0[0], p0[1], p1[0], p1[1]};
+        } else {
+            f.lo = *(const v4i *)(lds + at + (((2 * kk + h) * 16) ^ key));
+        }
+        if constexpr (EXACT) {
+            f.scale = *(const unsigned char *)(lds + scale_at) & b0;
+            f.scale1 = *(const unsigned char *)(lds + scale_at + 1) & b1;
+        } else {
+            f.scale = *(const unsigned char *)(lds + scale_at + h) & b0;
+        }
+    };
+    auto read_set = [&](Set &f, int kk, int step, int stage) __attribute__((always_inline)) {
+        const unsigned rows = (unsigned)stage * kStage;
+        const int block = (step * KK + kk) * 2;                        // the first of the two
+        const unsigned scales = (unsigned)(step / SPC % 3 * kChunk + (block & 15));
+        const unsigned b0 = block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, b1 = block + 1 < prm.nb ? 255u : 0u;
+#pragma unroll
+        for (int n = 0; n < TN; n++) read_rows(f.w[n], OW{}, rows + wlane + n * 32 * OW::kRow, wkey, scales + wslane + n * 512, kk, b0, b1);
+#pragma unroll
+        for (int m = 0; m < TM; m++) read_rows(f.x[m], OX{}, rows + xlane + m * 32 * OX::kRow, xkey, scales + xslane + m * 512, kk, b0, b1);
+    };
+    v16f acc[TN][TM] = {};
+    auto multiply = [&](const Set &f) __attribute__((always_inline)) {
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                auto bf16 = [&](const auto &g, bool wide) __attribute__((always_inline)) {
+                    const float s = __uint_as_float((i < 2 ? g.scale : g.scale1) << 23);
+                    const v4i q = wide && i >= 2 ? g.hi : g.lo;
+                    return wide ? bf16_of_mx8(q[2 * (i & 1)], q[2 * (i & 1) + 1], s) : bf16_of_mx4(q[i], s);
+                };
+                v8bf x[TM];
+#pragma unroll
+                for (int m = 0; m < TM; m++) x[m] = bf16(f.x[m], EX == kMx8);
+#pragma unroll
+                for (int n = 0; n < TN; n++) {
+                    const v8bf w = bf16(f.w[n], EW == kMx8);
+#pragma unroll
+                    for (int m = 0; m < TM; m++) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x[m], acc[n][m], 0, 0, 0);
+                }
+            }
+        } else {
+            constexpr int FW = EW == kMx8 ? 0 : 4, FX = EX == kMx8 ? 0 : 4;
+            auto codes = [](const v4i &lo, const v4i &hi, bool wide) __attribute__((always_inline)) {
+                return wide ? v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]} : v8i{lo[0], lo[1], lo[2], lo[3], 0, 0, 0, 0};
+            };
+#pragma unroll
+            for (int n = 0; n < TN; n++)
+#pragma unroll
+                for (int m = 0; m < TM; m++)
+                    acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(f.w[n].lo, f.w[n].hi, EW == kMx8), codes(f.x[m].lo, f.x[m].hi, EX == kMx8),
+                                                                                acc[n][m], FW, FX, 0, (int)f.w[n].scale, 0, (int)f.x[m].scale);
+        }
+    };
+    // completes this wavefront's LDS reads, waits for no vector-memory operation
+    auto ring_barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    const int steps = prm.steps;
+#pragma unroll
+    for (int j = 0; j < SPC * SL; j++) issue_scales(soff[j], j, 0);
+#pragma unroll
+    for (int i = 0; i < NST; i++) issue(i, i);
+    wait_loads<(NST - 1) * LPS>();
+    ring_barrier();
+    read_set(f0, 0, 0, 0);
+    read_set(f1, 1, 0, 0);
+
+    // The KK parts of a step: before the successors of the last but one are read the next step has arrived everywhere, and with that
+    // every wavefront has read the last part of this one, whose stage is filled again.  Steps past the last are all out of range:
+    // their loads bring zeros, touch no memory, and keep one form of the loop.
+    for (int i = 0, stage = 0; i < steps; i++) {
+        const int next = stage + 1 == NST ? 0 : stage + 1;
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+            Set &f = (kk & 1) ? f1 : f0;
+            multiply(f);
+            __builtin_amdgcn_sched_barrier(0);
+            if (kk == KK - 2) {
+                wait_loads<(NST - 2) * LPS>();
+                ring_barrier();
+            }
+            if (kk == KK - 1) issue(i + NST, stage);
+            if (kk + 2 < KK) read_set(f, kk + 2, i, stage);
+            else read_set(f, kk + 2 - KK, i + 1, next);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        stage = next;
+    }
+    wait_loads<0>();
+
+    // ---- results: lane holds features wn0 + 32n + 16h + 0..15 of token wm0 + 32m + l32.  32 tokens at a time go through the
+    // wavefront's own part of LDS, so that a row's features leave in whole cache lines, an octet to a lane.
+    constexpr int F = TN * 32, kPad = F + 4;
+    static_assert(NW * 32 * kPad * 4 <= NST * kStage + 3 * kChunk, "LDS for the results");
+    __syncthreads();                                                   // every wavefront has read its last operands
+    float *mine = (float *)lds + wave * 32 * kPad;
+#pragma unroll
+    for (int m = 0; m < TM; m++) {
+#pragma unroll
+        for (int n = 0; n < TN; n++)
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                *(v4f *)&mine[l32 * kPad + n * 32 + 16 * h + 4 * q] = v4f{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int i = lane; i < 32 * F / 8; i += 64) {
+            const int token = i / (F / 8), o = i % (F / 8);
+            const v4f *p = (const v4f *)&mine[token * kPad + o * 8];
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                v[j] = p[0][j];
+                v[4 + j] = p[1][j];
+            }
+            if (wm0 + m * 32 + token < mrows) finish_octet(v, a, m0 + wm0 + m * 32 + token, (n0 + wn0) / 8 + o);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int NST>
+hipError_t run(const LinearMxArgs &a, hipStream_t st)
+{
+    constexpr int KS = EX == kMx4 && EW == kMx4 ? 256 : 128;
+    constexpr int kLds = NST * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + 3 * (BM + BN) * 16;
+    static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
+    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN, NST>;
+    static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (allowed != hipSuccess) return allowed;
+    TileParams p{a, (a.K + kMxBlock - 1) / kMxBlock};
+    p.steps = (a.K + KS - 1) / KS;
+    p.tiles_n = (a.N + BN - 1) / BN;
+    // token rows of one launch: 2^31 tiles at most
+    const size_t most = (size_t)(0x7fffffff / p.tiles_n) * BM;
+    for (size_t m = 0; m < a.M; m += most) {
+        p.a = a;
+        advance_tokens(p.a, m);
+        p.a.M = a.M - m < most ? a.M - m : most;
+        p.tiles_m = (int)((p.a.M + BM - 1) / BM);
+        kernel<<<(unsigned)(p.tiles_m * p.tiles_n), WM * WN * 64, kLds, st>>>(p);
+    }
+    return hipGetLastError();
+}
+
+template <int EX, int EW, bool EXACT>
+hipError_t by_shape(const LinearMxArgs &a, hipStream_t st)
+{
+    return run<EX, EW, EXACT, 256, 256, 2, 4, 2>(a, st);
+}
+
+}  // namespace
+
+bool linear_mx_tiles_supports(const LinearMxArgs &a)
+{
+    // offsets inside a tile of 256 rows have 31 bits
+    constexpr size_t most = (size_t)1 << 22;
+    return a.ldx <= most && a.ldw <= most && a.ldxs <= most && a.ldws <= most;
+}
+
+hipError_t launch_linear_mx_tiles(const LinearMxArgs &a, hipStream_t st)
+{
+    const bool exact = !a.q.codes && a.dtype == kF32;
+    if (a.elem_x == kMx4 && a.elem_w == kMx4) return by_shape<kMx4, kMx4, false>(a, st);
+    if (a.elem_x == kMx4) return exact ? by_shape<kMx4, kMx8, true>(a, st) : by_shape<kMx4, kMx8, false>(a, st);
+    if (a.elem_w == kMx4) return exact ? by_shape<kMx8, kMx4, true>(a, st) : by_shape<kMx8, kMx4, false>(a, st);
+    return exact ? by_shape<kMx8, kMx8, true>(a, st) : by_shape<kMx8, kMx8, false>(a, st);
+}
+
+}  // namespace dfq
