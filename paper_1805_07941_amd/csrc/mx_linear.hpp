@@ -104,28 +104,44 @@ __device__ __forceinline__ v4f multiply16(const Frag16<EW, EXACT> &w, const Frag
     }
 }
 
-// Octet o (features 8o ..) of token m: bias, ReLU, rounding and the store.  Converted results: the four lanes of a quad hold a block.
-__device__ __forceinline__ void finish_octet(float (&v)[8], const LinearMxArgs &a, size_t m, int o)
-{
-    const int n = o * 8;
+// The end of results, an octet (features 8o .. 8o + 7) of one token at a time: bias, ReLU, rounding and the store.  A lane keeps its
+// octet from token to token.  Converted results: the four lanes of a quad hold a block and come here together.
+struct OctetEnd {
+    float bias[8];
+    int o, blocks;
+    bool vec;
+
+    __device__ __forceinline__ OctetEnd(const LinearMxArgs &a, int octet) : o(octet), blocks((a.N + kMxBlock - 1) / kMxBlock)
+    {
+        vec = ((uintptr_t)a.y | a.ldy * (a.dtype == kF32 ? 4 : 2)) % 16 == 0;
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-        if (a.bias && n + j < a.N) v[j] += a.bias[n + j];
-        if (a.relu) v[j] = relu_f32(v[j]);
+        for (int j = 0; j < 8; j++) bias[j] = a.bias && o * 8 + j < a.N ? a.bias[o * 8 + j] : 0.0f;
     }
-    if (a.q.codes) {
-        const int nb = (a.N + kMxBlock - 1) / kMxBlock;
-        if (o >= nb * 4) return;                                  // (whole quads)
+    __device__ __forceinline__ void put(float (&v)[8], const LinearMxArgs &a, size_t m) const
+    {
+        if (a.bias) {
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = n + j < a.N ? v[j] : 0.0f;
-        uint8_t *codes = a.q.codes + m * a.q.ldc, *scales = a.q.scales + m * a.q.lds;
-        if (a.q.elem == kMx8) mx_store_octet<kMx8>(v, codes, scales, o, nb, a.cover);
-        else mx_store_octet<kMx4>(v, codes, scales, o, nb, a.cover);
-    } else if (n < a.N) {
-        if (a.dtype == kF32) store_octet<kF32>(v, (char *)a.y + m * a.ldy * 4, o, a.N, ((uintptr_t)a.y | a.ldy * 4) % 16 == 0);
-        else if (a.dtype == kBF16) store_octet<kBF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, ((uintptr_t)a.y | a.ldy * 2) % 16 == 0);
-        else store_octet<kF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, ((uintptr_t)a.y | a.ldy * 2) % 16 == 0);
+            for (int j = 0; j < 8; j++) v[j] += bias[j];
+        }
+        if (a.relu) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = relu_f32(v[j]);
+        }
+        if (a.q.codes) {
+            if (o >= blocks * 4) return;                          // (whole quads)
+            if (o * 8 + 8 > a.N) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[j] = o * 8 + j < a.N ? v[j] : 0.0f;
+            }
+            uint8_t *codes = a.q.codes + m * a.q.ldc, *scales = a.q.scales + m * a.q.lds;
+            if (a.q.elem == kMx8) mx_store_octet<kMx8>(v, codes, scales, o, blocks, a.cover);
+            else mx_store_octet<kMx4>(v, codes, scales, o, blocks, a.cover);
+        } else if (o * 8 < a.N) {
+            if (a.dtype == kF32) store_octet<kF32>(v, (char *)a.y + m * a.ldy * 4, o, a.N, vec);
+            else if (a.dtype == kBF16) store_octet<kBF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, vec);
+            else store_octet<kF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, vec);
+        }
     }
-}
+};
 
 }  // namespace dfq

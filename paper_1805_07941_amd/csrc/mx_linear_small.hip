@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a
                 v[4 + j] += p[1][j];
             }
         }
-        if (m < a.M) finish_octet(v, a, m, n0 / 8 + o);
+        if (m < a.M) OctetEnd(a, n0 / 8 + o).put(v, a, m);
     }
 }
 

@@ -4,7 +4,7 @@
 // second; feature rows lie in LDS in an order that leaves 16 consecutive features of one token in each lane.  A workgroup walks the
 // reduction axis in steps of 128 bytes of an operand row (256 values of 4 bits, 128 where an operand has 8) through a ring of LDS
 // stages that direct global -> LDS loads fill, one barrier to a step.  A wavefront waits for its own loads of the step it is about to
-// read only, and reads the operands of the instruction after next while the matrix pipe is busy with this one.
+// read only, and reads the next 64 values' operands while the matrix pipe is busy with these.
 //
 // Scales come in chunks of 16 bytes of a row (512 values): a row's four bytes of one step would cost as many cache lines as its 128
 // bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c; three buffers, because loads run NST steps ahead of
@@ -40,6 +40,9 @@ struct Operand {
     // physical place of a row's logical piece: 16 consecutive rows put one piece on all banks
     __device__ static __forceinline__ int place(int row, int piece) { return kRow == 128 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3); }
 };
+
+// where a row's words of a chunk of scales are
+__device__ __forceinline__ int scale_key(int row) { return (row >> 3) & 3; }
 
 // One lane's operands of a 32-row group for 64 values: what v_mfma_scale_f32_32x32x64_f8f6f4 wants (with h = lane / 32: of 4-bit
 // elements block h, of 8-bit ones bytes 16h.. of both blocks), and block h's scale byte.  EXACT: bytes 16h.. (4 bits: 8h..) of both
@@ -100,40 +103,28 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // feature of LDS row r of the weights (within the tile): row 8g + 4h + e of a group of 32 holds feature 16h + 4g + e
     auto feature_of = [](int r) { return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r & 31) >> 3) + (r & 3); };
 
-    // ---- producer: a wavefront-wide load fills 1024 bytes of a stage, rows lane / pieces of it; the lane's logical piece is the same
-    // in every load (the number of wavefronts is even)
+    // ---- producer: a wavefront-wide load fills 1024 bytes of a stage, rows lane / pieces of it.  From one load of a wavefront to its
+    // next the lane's logical piece stays the same (the number of wavefronts is even) and its row, a feature's too, moves by a
+    // multiple of 32: one offset in a register serves them all.  Rows past the last lie behind the buffer's end by themselves.
     constexpr int XR = 64 / OX::kPieces16, WR = 64 / OW::kPieces16;    // rows of a load
+    static_assert(XR * NW % 32 == 0 && WR * NW % 32 == 0 && 16 * NW % 32 == 0, "rows from load to load");
     const int xp = OX::place(XR * wave + lane / OX::kPieces16, lane % OX::kPieces16) * 16;
     const int wp = OW::place(WR * wave + lane / OW::kPieces16, lane % OW::kPieces16) * 16;
-    unsigned xoff[XL], woff[WL], soff[SPC * SL];
-#pragma unroll
-    for (int j = 0; j < XL; j++) {
-        const int r = XR * (wave + NW * j) + lane / OX::kPieces16;
-        xoff[j] = r < mrows ? (unsigned)r * ldx + xp : kOutOfRange;
-    }
-#pragma unroll
-    for (int j = 0; j < WL; j++) {
-        const int n = feature_of(WR * (wave + NW * j) + lane / OW::kPieces16);
-        woff[j] = n < nrows ? (unsigned)n * ldw + wp : kOutOfRange;
-    }
-    // scales: a load fills 16 rows of a chunk, rows 0 .. BM-1 the tokens', then the features' in their LDS order
-    static_assert(BM % 16 == 0, "a load of scales has rows of one operand");
-#pragma unroll
-    for (int j = 0; j < SPC * SL; j++) {
-        const int first = 16 * (wave + NW * j), r = first + lane / 4;
-        if (first < BM) {
-            soff[j] = r < mrows ? (unsigned)r * ldxs + (lane & 3) * 4 : kOutOfRange;
-        } else {
-            const int n = feature_of(r - BM);
-            soff[j] = n < nrows ? (unsigned)n * ldws + (lane & 3) * 4 : kOutOfRange;
-        }
-    }
-    auto issue_scales = [&](unsigned off, int j, int chunk) __attribute__((always_inline)) {
-        const int first = 16 * (wave + NW * j);
-        const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds_base + NST * kStage + (unsigned)(chunk % 3) * kChunk + (unsigned)first * 16));
-        const bool x = first < BM;
+    const unsigned xoff = (unsigned)(XR * wave + lane / OX::kPieces16) * ldx + xp;
+    const unsigned woff = (unsigned)feature_of(WR * wave + lane / OW::kPieces16) * ldw + wp;
+    // scales: a load fills 16 rows of a chunk, rows 0 .. BM-1 the tokens', then the features' in their LDS order.  Which of a row's
+    // four words a lane brings is XOR-ed with bits of the row, so that one word of 32 rows lies on 32 banks.
+    static_assert(BM % (16 * NW) == 0 && BN % (16 * NW) == 0, "a load of scales has rows of one operand");
+    const unsigned sword = (unsigned)((lane & 3) ^ scale_key(16 * wave + lane / 4)) * 4;
+    const unsigned xsoff = (unsigned)(16 * wave + lane / 4) * ldxs + sword, wsoff = (unsigned)feature_of(16 * wave + lane / 4) * ldws + sword;
+    // load j of a chunk
+    auto issue_scales = [&](int j, int chunk) __attribute__((always_inline)) {
+        const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane(
+            (int)(lds_base + NST * kStage + (unsigned)(chunk % 3) * kChunk + (unsigned)(wave + NW * j) * 256u));
+        const bool x = j < BM / (16 * NW);
         const v4i r = {x ? xsr.x : wsr.x, x ? xsr.y : wsr.y, x ? xsr.z : wsr.z, wsr.w};
-        load_word_to_lds(off + (unsigned)chunk * 16, r, dst);
+        const unsigned moved = x ? (unsigned)j * (16 * NW) * ldxs : (unsigned)(j - BM / (16 * NW)) * (16 * NW) * ldws;
+        load_word_to_lds((x ? xsoff : wsoff) + (moved + (unsigned)chunk * 16), r, dst);
     };
     // (without a branch: the compiler would sink the matrix instructions in front of one behind it)
     auto issue = [&](int step, int stage) __attribute__((always_inline)) {
@@ -141,29 +132,21 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
         const unsigned kx = (unsigned)step * OX::kRow, kw = (unsigned)step * OW::kRow;
         const unsigned badx = kx + xp < xrow ? 0u : kOutOfRange, badw = kw + wp < wrow ? 0u : kOutOfRange;
 #pragma unroll
-        for (int j = 0; j < XL; j++) load_piece_to_lds((xoff[j] + kx) | badx, xr, base + (unsigned)j * (NW * 1024u));
+        for (int j = 0; j < XL; j++) load_piece_to_lds((xoff + (kx + j * (XR * NW) * ldx)) | badx, xr, base + (unsigned)j * (NW * 1024u));
 #pragma unroll
-        for (int j = 0; j < WL; j++) load_piece_to_lds((woff[j] + kw) | badw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
-        const int part = step % SPC, chunk = step / SPC + 1;
+        for (int j = 0; j < WL; j++) load_piece_to_lds((woff + (kw + j * (WR * NW) * ldw)) | badw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
 #pragma unroll
-        for (int j = 0; j < SL; j++) {
-            unsigned off = soff[j];
-#pragma unroll
-            for (int p = 1; p < SPC; p++) off = part == p ? soff[p * SL + j] : off;
-            issue_scales(off, part * SL + j, chunk);
-        }
+        for (int j = 0; j < SL; j++) issue_scales(step % SPC * SL + j, step / SPC + 1);
     };
 
     // ---- consumer
     const int wm0 = wave % WM * (BM / WM), wn0 = wave / WM * (BN / WN);
-    struct Set {
-        Frag32<EW, EXACT> w[TN];
-        Frag32<EX, EXACT> x[TM];
-    };
-    Set f0, f1;
+    Frag32<EW, EXACT> fw[2][TN];                                       // this part's and the next one's
+    Frag32<EX, EXACT> fx[TM];                                          // each read again as soon as it is multiplied
     // Addresses: a lane's row and the key of its pieces are the same in every group of 32 rows; the groups differ by constants.
     const unsigned xlane = (unsigned)(wm0 + l32) * OX::kRow, wlane = (unsigned)(BM * OX::kRow + (wn0 + l32) * OW::kRow);
     const unsigned xkey = OX::place(l32, 0) * 16, wkey = OW::place(l32, 0) * 16;
+    const unsigned skey = scale_key(l32) * 4;
     const unsigned xslane = (unsigned)(NST * kStage + (wm0 + l32) * 16), wslane = (unsigned)(NST * kStage + (BM + wn0 + l32) * 16);
     auto read_rows = [&](auto &f, auto op, unsigned at, unsigned key, unsigned scale_at, int kk, unsigned b0, unsigned b1) __attribute__((always_inline)) {
         constexpr bool wide = decltype(op)::kRow * 8 / KS == 8;
@@ -184,35 +167,35 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
             f.scale = *(const unsigned char *)(lds + scale_at + h) & b0;
         }
     };
-    auto read_set = [&](Set &f, int kk, int step, int stage) __attribute__((always_inline)) {
-        const unsigned rows = (unsigned)stage * kStage;
+    struct Part {                                                      // 64 values of the reduction axis
+        int kk;
+        unsigned rows, scales, b0, b1;
+    };
+    auto part_of = [&](int step, int stage, int kk) __attribute__((always_inline)) {
         const int block = (step * KK + kk) * 2;                        // the first of the two
-        const unsigned scales = (unsigned)(step / SPC % 3 * kChunk + (block & 15));
-        const unsigned b0 = block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, b1 = block + 1 < prm.nb ? 255u : 0u;
-#pragma unroll
-        for (int n = 0; n < TN; n++) read_rows(f.w[n], OW{}, rows + wlane + n * 32 * OW::kRow, wkey, scales + wslane + n * 512, kk, b0, b1);
-#pragma unroll
-        for (int m = 0; m < TM; m++) read_rows(f.x[m], OX{}, rows + xlane + m * 32 * OX::kRow, xkey, scales + xslane + m * 512, kk, b0, b1);
+        return Part{kk, (unsigned)stage * kStage, (unsigned)(step / SPC % 3 * kChunk) + ((unsigned)(block & 12) ^ skey) + (unsigned)(block & 2),
+                    block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, block + 1 < prm.nb ? 255u : 0u};
+    };
+    auto read_w = [&](Frag32<EW, EXACT> &f, int n, const Part &p) __attribute__((always_inline)) {
+        read_rows(f, OW{}, p.rows + wlane + n * 32 * OW::kRow, wkey, p.scales + wslane + n * 512, p.kk, p.b0, p.b1);
+    };
+    auto read_x = [&](int m, const Part &p) __attribute__((always_inline)) {
+        read_rows(fx[m], OX{}, p.rows + xlane + m * 32 * OX::kRow, xkey, p.scales + xslane + m * 512, p.kk, p.b0, p.b1);
     };
     v16f acc[TN][TM] = {};
-    auto multiply = [&](const Set &f) __attribute__((always_inline)) {
+    auto multiply = [&](const Frag32<EW, EXACT> (&w)[TN], int m) __attribute__((always_inline)) {
+        const auto &x = fx[m];
         if constexpr (EXACT) {
+            auto bf16 = [&](const auto &g, bool wide, int i) __attribute__((always_inline)) {
+                const float s = __uint_as_float((i < 2 ? g.scale : g.scale1) << 23);
+                const v4i q = wide && i >= 2 ? g.hi : g.lo;
+                return wide ? bf16_of_mx8(q[2 * (i & 1)], q[2 * (i & 1) + 1], s) : bf16_of_mx4(q[i], s);
+            };
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                auto bf16 = [&](const auto &g, bool wide) __attribute__((always_inline)) {
-                    const float s = __uint_as_float((i < 2 ? g.scale : g.scale1) << 23);
-                    const v4i q = wide && i >= 2 ? g.hi : g.lo;
-                    return wide ? bf16_of_mx8(q[2 * (i & 1)], q[2 * (i & 1) + 1], s) : bf16_of_mx4(q[i], s);
-                };
-                v8bf x[TM];
+                const v8bf xb = bf16(x, EX == kMx8, i);
 #pragma unroll
-                for (int m = 0; m < TM; m++) x[m] = bf16(f.x[m], EX == kMx8);
-#pragma unroll
-                for (int n = 0; n < TN; n++) {
-                    const v8bf w = bf16(f.w[n], EW == kMx8);
-#pragma unroll
-                    for (int m = 0; m < TM; m++) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x[m], acc[n][m], 0, 0, 0);
-                }
+                for (int n = 0; n < TN; n++) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16(w[n], EW == kMx8, i), xb, acc[n][m], 0, 0, 0);
             }
         } else {
             constexpr int FW = EW == kMx8 ? 0 : 4, FX = EX == kMx8 ? 0 : 4;
@@ -221,10 +204,8 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
             };
 #pragma unroll
             for (int n = 0; n < TN; n++)
-#pragma unroll
-                for (int m = 0; m < TM; m++)
-                    acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(f.w[n].lo, f.w[n].hi, EW == kMx8), codes(f.x[m].lo, f.x[m].hi, EX == kMx8),
-                                                                                acc[n][m], FW, FX, 0, (int)f.w[n].scale, 0, (int)f.x[m].scale);
+                acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n].lo, w[n].hi, EW == kMx8), codes(x.lo, x.hi, EX == kMx8), acc[n][m], FW, FX, 0,
+                                                                            (int)w[n].scale, 0, (int)x.scale);
         }
     };
     // completes this wavefront's LDS reads, waits for no vector-memory operation
@@ -232,32 +213,44 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
 
     const int steps = prm.steps;
 #pragma unroll
-    for (int j = 0; j < SPC * SL; j++) issue_scales(soff[j], j, 0);
+    for (int j = 0; j < SPC * SL; j++) issue_scales(j, 0);
 #pragma unroll
     for (int i = 0; i < NST; i++) issue(i, i);
     wait_loads<(NST - 1) * LPS>();
     ring_barrier();
-    read_set(f0, 0, 0, 0);
-    read_set(f1, 1, 0, 0);
+    {
+        const Part p = part_of(0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < TN; n++) read_w(fw[0][n], n, p);
+#pragma unroll
+        for (int m = 0; m < TM; m++) read_x(m, p);
+    }
 
-    // The KK parts of a step: before the successors of the last but one are read the next step has arrived everywhere, and with that
-    // every wavefront has read the last part of this one, whose stage is filled again.  Steps past the last are all out of range:
+    // A step's KK parts.  A token group's operands are read again for the next part as soon as they are multiplied, the features'
+    // into the other of two sets.  Behind the first products of a step's last part every read of this step has been made: the
+    // wavefronts meet there, the next step having arrived, and the stage is filled again.  Steps past the last are all out of range:
     // their loads bring zeros, touch no memory, and keep one form of the loop.
     for (int i = 0, stage = 0; i < steps; i++) {
         const int next = stage + 1 == NST ? 0 : stage + 1;
 #pragma unroll
         for (int kk = 0; kk < KK; kk++) {
-            Set &f = (kk & 1) ? f1 : f0;
-            multiply(f);
-            __builtin_amdgcn_sched_barrier(0);
-            if (kk == KK - 2) {
-                wait_loads<(NST - 2) * LPS>();
-                ring_barrier();
+            const Part p = kk + 1 < KK ? part_of(i, stage, kk + 1) : part_of(i + 1, next, 0);
+#pragma unroll
+            for (int m = 0; m < TM; m++) {
+                multiply(fw[kk & 1], m);
+                __builtin_amdgcn_sched_barrier(0);
+                if (m == 0) {
+                    if (kk == KK - 1) {
+                        wait_loads<(NST - 2) * LPS>();
+                        ring_barrier();
+                    }
+#pragma unroll
+                    for (int n = 0; n < TN; n++) read_w(fw[~kk & 1][n], n, p);
+                }
+                read_x(m, p);
+                if (kk == KK - 1 && m == (KK == 2 ? 1 : TM - 1)) issue(i + NST, stage);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (kk == KK - 1) issue(i + NST, stage);
-            if (kk + 2 < KK) read_set(f, kk + 2, i, stage);
-            else read_set(f, kk + 2 - KK, i + 1, next);
-            __builtin_amdgcn_sched_barrier(0);
         }
         stage = next;
     }
@@ -269,25 +262,31 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     static_assert(NW * 32 * kPad * 4 <= NST * kStage + 3 * kChunk, "LDS for the results");
     __syncthreads();                                                   // every wavefront has read its last operands
     float *mine = (float *)lds + wave * 32 * kPad;
-#pragma unroll
+    constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
+    const OctetEnd end(a, (n0 + wn0) / 8 + lane % kOctets);
+#pragma unroll 1
     for (int m = 0; m < TM; m++) {
 #pragma unroll
-        for (int n = 0; n < TN; n++)
+        for (int mm = 0; mm < TM; mm++) {
+            if (mm != m) continue;
 #pragma unroll
-            for (int q = 0; q < 4; q++)
-                *(v4f *)&mine[l32 * kPad + n * 32 + 16 * h + 4 * q] = v4f{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+            for (int n = 0; n < TN; n++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    *(v4f *)&mine[l32 * kPad + n * 32 + 16 * h + 4 * q] = v4f{acc[n][mm][4 * q], acc[n][mm][4 * q + 1], acc[n][mm][4 * q + 2], acc[n][mm][4 * q + 3]};
+        }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-        for (int i = lane; i < 32 * F / 8; i += 64) {
-            const int token = i / (F / 8), o = i % (F / 8);
-            const v4f *p = (const v4f *)&mine[token * kPad + o * 8];
+        for (int it = 0; it < 32; it += kTokens) {
+            const int token = it + lane / kOctets;
+            const v4f *p = (const v4f *)&mine[token * kPad + lane % kOctets * 8];
             float v[8];
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 v[j] = p[0][j];
                 v[4 + j] = p[1][j];
             }
-            if (wm0 + m * 32 + token < mrows) finish_octet(v, a, m0 + wm0 + m * 32 + token, (n0 + wn0) / 8 + o);
+            if (wm0 + m * 32 + token < mrows) end.put(v, a, m0 + wm0 + m * 32 + token);
         }
         __builtin_amdgcn_wave_barrier();
     }
