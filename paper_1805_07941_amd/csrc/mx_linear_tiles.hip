@@ -2,12 +2,12 @@
 //
 // acc[n][m] = sum_k w[n][k] * x[m][k]: features are the rows of the matrix instruction's first operand and tokens the columns of its
 // second; feature rows lie in LDS in an order that leaves 16 consecutive features of one token in each lane.  A workgroup walks the
-// reduction axis in steps of 128 bytes of an operand row (256 values of 4 bits, 128 where an operand has 8) through a ring of LDS
-// stages that direct global -> LDS loads fill, one barrier to a step.  A wavefront waits for its own loads of the step it is about to
+// reduction axis in steps of 128 bytes of an operand row (256 values of 4 bits, 128 where an operand has 8) through two LDS stages
+// that direct global -> LDS loads fill, one barrier to a step.  A wavefront waits for its own loads of the step it is about to
 // read only, and reads the next 64 values' operands while the matrix pipe is busy with these.
 //
 // Scales come in chunks of 16 bytes of a row (512 values): a row's four bytes of one step would cost as many cache lines as its 128
-// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c; three buffers, because loads run NST steps ahead of
+// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c; three buffers, because loads run two steps ahead of
 // the reads.  What lies behind a row's last block is masked twice: codes by an offset past the buffer (zeros arrive), scales by a
 // comparison when they are read, so that neither the next row's bytes nor padding count.
 #include "conv_ring.hpp"
@@ -32,6 +32,16 @@ __device__ __forceinline__ void load_word_to_lds(unsigned voffset, v4i rsrc, uns
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voffset), "s"(rsrc), "s"(lds_base) : "memory", "m0");
 }
 
+// f(0), f(1), .. f(N - 1) with the number as a type
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void static_for(F &&f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, I + 1>(f);
+    }
+}
+
 template <int ELEM, int KS>
 struct Operand {
     static constexpr int kRow = KS * (ELEM == kMx8 ? 8 : 4) / 8;      // bytes of a row in a stage
@@ -53,7 +63,7 @@ struct Frag32 {
     unsigned scale, scale1;
 };
 
-template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int NST>
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_kernel(TileParams prm)
 {
     constexpr int NW = WM * WN;
@@ -67,12 +77,11 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     constexpr int SL = (BM + BN) / 16 / SPC / NW;                      // scale loads of a wavefront in a step
     static_assert(XL * NW * 1024 == BM * OX::kRow && WL * NW * 1024 == BN * OW::kRow && SL * SPC * NW * 16 == BM + BN, "whole loads");
     constexpr int LPS = XL + WL + SL;
-    static_assert(NST >= 2 && NST <= SPC + 1, "three chunks of scales");
-    static_assert(NST * LPS < 64 && SPC * SL + NST * LPS < 64, "outstanding loads fit the counter");
+    static_assert(SPC * SL + 2 * LPS < 64, "outstanding loads fit the counter");
     constexpr int kStage = BM * OX::kRow + BN * OW::kRow;
     constexpr int kChunk = (BM + BN) * 16;
 
-    extern __shared__ char lds[];                                      // NST stages, then three chunks of scales
+    extern __shared__ char lds[];                                      // two stages, then three chunks of scales
     const LinearMxArgs &a = prm.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h = lane >> 5;
@@ -120,24 +129,37 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // load j of a chunk
     auto issue_scales = [&](int j, int chunk) __attribute__((always_inline)) {
         const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane(
-            (int)(lds_base + NST * kStage + (unsigned)(chunk % 3) * kChunk + (unsigned)(wave + NW * j) * 256u));
+            (int)(lds_base + 2 * kStage + (unsigned)(chunk % 3) * kChunk + (unsigned)(wave + NW * j) * 256u));
         const bool x = j < BM / (16 * NW);
         const v4i r = {x ? xsr.x : wsr.x, x ? xsr.y : wsr.y, x ? xsr.z : wsr.z, wsr.w};
         const unsigned moved = x ? (unsigned)j * (16 * NW) * ldxs : (unsigned)(j - BM / (16 * NW)) * (16 * NW) * ldws;
         load_word_to_lds((x ? xsoff : wsoff) + (moved + (unsigned)chunk * 16), r, dst);
     };
-    // (without a branch: the compiler would sink the matrix instructions in front of one behind it)
-    auto issue = [&](int step, int stage) __attribute__((always_inline)) {
+    // loads FROM .. TO-1 of a wavefront's LPS for a step (without a branch: the compiler would sink the matrix instructions in front of
+    // one behind it)
+    auto issue = [&](int step, int stage, auto from, auto to) __attribute__((always_inline)) {
+        constexpr int kFrom = decltype(from)::value, kTo = decltype(to)::value;
         const unsigned base = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds_base + (unsigned)stage * kStage + (unsigned)wave * 1024u));
         const unsigned kx = (unsigned)step * OX::kRow, kw = (unsigned)step * OW::kRow;
         const unsigned badx = kx + xp < xrow ? 0u : kOutOfRange, badw = kw + wp < wrow ? 0u : kOutOfRange;
 #pragma unroll
-        for (int j = 0; j < XL; j++) load_piece_to_lds((xoff + (kx + j * (XR * NW) * ldx)) | badx, xr, base + (unsigned)j * (NW * 1024u));
-#pragma unroll
-        for (int j = 0; j < WL; j++) load_piece_to_lds((woff + (kw + j * (WR * NW) * ldw)) | badw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
-#pragma unroll
-        for (int j = 0; j < SL; j++) issue_scales(step % SPC * SL + j, step / SPC + 1);
+        for (int q = kFrom; q < kTo; q++) {
+            const int j = q < XL ? q : q < XL + WL ? q - XL : q - XL - WL;
+            if (q < XL) load_piece_to_lds((xoff + (kx + j * (XR * NW) * ldx)) | badx, xr, base + (unsigned)j * (NW * 1024u));
+            else if (q < XL + WL) load_piece_to_lds((woff + (kw + j * (WR * NW) * ldw)) | badw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
+            else issue_scales(step % SPC * SL + j, step / SPC + 1);
+        }
     };
+    // A step's loads are issued one or two at a time between matrix instructions - a burst of them fills the memory pipeline's queue and
+    // holds up the wavefront - from slot 0 behind the barrier that frees the stage on: over the rest of the step's last part, and with
+    // four parts to a step over the first part of the next step too.  (EXACT: registers for one burst only.)
+    constexpr int kLate = EXACT || TM == 1 ? 1 : TM - 1, kSlots = kLate + (KK == 4 && !EXACT ? TM : 0);
+    auto issue_slot = [&](int step, int stage, auto slot) __attribute__((always_inline)) {
+        constexpr int s = decltype(slot)::value;
+        issue(step, stage, std::integral_constant<int, s * LPS / kSlots>{}, std::integral_constant<int, (s + 1) * LPS / kSlots>{});
+    };
+    constexpr int kFirst = kLate * LPS / kSlots;                       // loads of a step issued before the next one begins
+    using None = std::integral_constant<int, 0>;
 
     // ---- consumer
     const int wm0 = wave % WM * (BM / WM), wn0 = wave / WM * (BN / WN);
@@ -147,7 +169,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     const unsigned xlane = (unsigned)(wm0 + l32) * OX::kRow, wlane = (unsigned)(BM * OX::kRow + (wn0 + l32) * OW::kRow);
     const unsigned xkey = OX::place(l32, 0) * 16, wkey = OW::place(l32, 0) * 16;
     const unsigned skey = scale_key(l32) * 4;
-    const unsigned xslane = (unsigned)(NST * kStage + (wm0 + l32) * 16), wslane = (unsigned)(NST * kStage + (BM + wn0 + l32) * 16);
+    const unsigned xslane = (unsigned)(2 * kStage + (wm0 + l32) * 16), wslane = (unsigned)(2 * kStage + (BM + wn0 + l32) * 16);
     auto read_rows = [&](auto &f, auto op, unsigned at, unsigned key, unsigned scale_at, int kk, unsigned b0, unsigned b1) __attribute__((always_inline)) {
         constexpr bool wide = decltype(op)::kRow * 8 / KS == 8;
         if constexpr (wide) {
@@ -214,9 +236,9 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     const int steps = prm.steps;
 #pragma unroll
     for (int j = 0; j < SPC * SL; j++) issue_scales(j, 0);
-#pragma unroll
-    for (int i = 0; i < NST; i++) issue(i, i);
-    wait_loads<(NST - 1) * LPS>();
+    issue(0, 0, None{}, std::integral_constant<int, LPS>{});
+    issue(1, 1, None{}, std::integral_constant<int, kFirst>{});
+    wait_loads<kFirst>();
     ring_barrier();
     {
         const Part p = part_of(0, 0, 0);
@@ -231,27 +253,29 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // wavefronts meet there, the next step having arrived, and the stage is filled again.  Steps past the last are all out of range:
     // their loads bring zeros, touch no memory, and keep one form of the loop.
     for (int i = 0, stage = 0; i < steps; i++) {
-        const int next = stage + 1 == NST ? 0 : stage + 1;
-#pragma unroll
-        for (int kk = 0; kk < KK; kk++) {
+        const int next = stage ^ 1;
+        static_for<KK>([&](auto part) __attribute__((always_inline)) {
+            constexpr int kk = decltype(part)::value;
             const Part p = kk + 1 < KK ? part_of(i, stage, kk + 1) : part_of(i + 1, next, 0);
-#pragma unroll
-            for (int m = 0; m < TM; m++) {
+            static_for<TM>([&](auto group) __attribute__((always_inline)) {
+                constexpr int m = decltype(group)::value;
                 multiply(fw[kk & 1], m);
                 __builtin_amdgcn_sched_barrier(0);
-                if (m == 0) {
-                    if (kk == KK - 1) {
-                        wait_loads<(NST - 2) * LPS>();
+                if constexpr (m == 0) {
+                    if constexpr (kk == KK - 1) {
+                        wait_loads<0>();
                         ring_barrier();
                     }
 #pragma unroll
                     for (int n = 0; n < TN; n++) read_w(fw[~kk & 1][n], n, p);
                 }
                 read_x(m, p);
-                if (kk == KK - 1 && m == (KK == 2 ? 1 : TM - 1)) issue(i + NST, stage);
+                constexpr int late = TM == 1 ? m : m - 1;
+                if constexpr (kk == KK - 1 && late >= 0 && late < kLate) issue_slot(i + 2, stage, std::integral_constant<int, late < 0 ? 0 : late>{});
+                if constexpr (kk == 0 && kSlots > kLate) issue_slot(i + 1, next, std::integral_constant<int, kLate + m>{});
                 __builtin_amdgcn_sched_barrier(0);
-            }
-        }
+            });
+        });
         stage = next;
     }
     wait_loads<0>();
@@ -259,7 +283,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // ---- results: lane holds features wn0 + 32n + 16h + 0..15 of token wm0 + 32m + l32.  32 tokens at a time go through the
     // wavefront's own part of LDS, so that a row's features leave in whole cache lines, an octet to a lane.
     constexpr int F = TN * 32, kPad = F + 4;
-    static_assert(NW * 32 * kPad * 4 <= NST * kStage + 3 * kChunk, "LDS for the results");
+    static_assert(NW * 32 * kPad * 4 <= 2 * kStage + 3 * kChunk, "LDS for the results");
     __syncthreads();                                                   // every wavefront has read its last operands
     float *mine = (float *)lds + wave * 32 * kPad;
     constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
@@ -292,13 +316,13 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     }
 }
 
-template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int NST>
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN>
 hipError_t run(const LinearMxArgs &a, hipStream_t st)
 {
     constexpr int KS = EX == kMx4 && EW == kMx4 ? 256 : 128;
-    constexpr int kLds = NST * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + 3 * (BM + BN) * 16;
+    constexpr int kLds = 2 * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + 3 * (BM + BN) * 16;
     static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
-    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN, NST>;
+    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN>;
     static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (allowed != hipSuccess) return allowed;
     TileParams p{a, (a.K + kMxBlock - 1) / kMxBlock};
@@ -319,7 +343,7 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
 template <int EX, int EW, bool EXACT>
 hipError_t by_shape(const LinearMxArgs &a, hipStream_t st)
 {
-    return run<EX, EW, EXACT, 256, 256, 2, 4, 2>(a, st);
+    return run<EX, EW, EXACT, 256, 256, 2, 4>(a, st);
 }
 
 }  // namespace
