@@ -151,6 +151,19 @@ dfq_status dfq_linear_mx_q(const uint8_t *x, size_t ldx, const uint8_t *x_scales
                            const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, uint8_t *codes, size_t ldc,
                            uint8_t *scales, size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream);
 
+/* Either of the two (y, or codes and scales; the other NULL) by a kernel chosen by the caller (tests, benchmarks).  A workgroup has
+ * tokens x features as the name says; the STREAM forms share the reduction between its wavefronts, the TILE forms its operands.
+ * DFQ_EUNSUPPORTED if that kernel cannot run the call: rows of an operand more than 2^22 bytes apart take DFQ_LINEAR_DIRECT, converted
+ * results no DFQ_LINEAR_STREAM_16X16. */
+typedef enum {
+    DFQ_LINEAR_AUTO = 0, DFQ_LINEAR_DIRECT = 1, DFQ_LINEAR_STREAM_16X16 = 2, DFQ_LINEAR_STREAM_16X32 = 3, DFQ_LINEAR_STREAM_32X32 = 4,
+    DFQ_LINEAR_STREAM_32X64 = 5, DFQ_LINEAR_TILE_64X64 = 6, DFQ_LINEAR_TILE_128X128 = 7, DFQ_LINEAR_TILE_256X256 = 8
+} dfq_linear_variant;
+dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs,
+                                 dfq_mx_elem elem_x, const uint8_t *w, size_t ldw, const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w,
+                                 const float *bias, void *y, size_t ldy, dfq_dtype dtype, uint8_t *codes, size_t ldc, uint8_t *scales,
+                                 size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream);
+
 /* Root-mean-square norm with the addition in front of it and the conversion behind it, row by row, in float32:
  *   s = x + add;  v = s / sqrt(mean(s^2) + eps) * weight;  sum = s rounded to dtype;  y = v rounded to dtype;  codes, scales = v converted
  * add, sum, weight (NULL: ones), y and codes may be NULL, y and codes not both; the norm reads s unrounded.  x, add, sum and y are rows

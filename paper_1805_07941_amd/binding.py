@@ -22,6 +22,9 @@ OK, EINVAL, ESHAPE, EFMT, EUNSUPPORTED, EDEVICE = range(6)
 POOL_MAX, POOL_AVG = 0, 1
 MX4, MX8 = 0, 1               # dfq_mx_elem
 MX_COVER, MX_FLOOR = 0, 1     # dfq_mx_rule
+LINEAR_AUTO, LINEAR_DIRECT = 0, 1      # dfq_linear_variant: these, and kernels by the tokens x features of a workgroup
+LINEAR_VARIANT_NAMES = {LINEAR_AUTO: "auto", LINEAR_DIRECT: "direct", 2: "stream 16x16", 3: "stream 16x32", 4: "stream 32x32", 5: "stream 32x64",
+                        6: "tile 64x64", 7: "tile 128x128", 8: "tile 256x256"}
 MX_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # dfq_dtype
 CAL_AMAX_WORDS = 256          # DFQ_CAL_AMAX_WORDS
 CALL_ARGS = 30                # DFQ_CALL_ARGS
@@ -40,7 +43,7 @@ EXPORTS = [
     "dfq_cal_weights", "dfq_cal_quantize", "dfq_cal_rescale", "dfq_cal_add", "dfq_cal_concat",
     "dfq_cal_np_weights", "dfq_cal_np_quantize", "dfq_cal_conv_np", "dfq_cal_add_np",
     "dfq_conv_np_absmax", "dfq_eltwise_np_absmax", "dfq_np_frac_from_absmax_u64", "dfq_pool_np", "dfq_stem_pack_x", "dfq_stem_pack_w", "dfq_conv_np_add",
-    "dfq_quantize_mx", "dfq_dequantize_mx", "dfq_linear_mx", "dfq_linear_mx_q", "dfq_rms_norm_mx",
+    "dfq_quantize_mx", "dfq_dequantize_mx", "dfq_linear_mx", "dfq_linear_mx_q", "dfq_linear_mx_variant", "dfq_rms_norm_mx",
     "dfq_conv_q_maxpool", "dfq_quantize_conv_q_maxpool", "dfq_conv_q_pc_maxpool", "dfq_quantize_conv_q_pc_maxpool", "dfq_quantize_conv_q",
 ]
 
@@ -157,8 +160,9 @@ def lib():
     linear_args = [vp, sz, vp, sz, i32] * 2 + [vp]
     L.dfq_linear_mx.argtypes = linear_args + [vp, sz, i32, sz, i32, i32, i32, vp]
     L.dfq_linear_mx_q.argtypes = linear_args + [vp, sz, vp, sz, i32, i32, sz, i32, i32, i32, vp]
+    L.dfq_linear_mx_variant.argtypes = [i32] + linear_args + [vp, sz, i32, vp, sz, vp, sz, i32, i32, sz, i32, i32, i32, vp]
     L.dfq_rms_norm_mx.argtypes = [vp, sz, vp, sz, vp, sz, i32, vp, i32, C.c_float, vp, sz, vp, sz, vp, sz, i32, i32, sz, i32, vp]
-    for name in ("dfq_quantize_mx", "dfq_dequantize_mx", "dfq_linear_mx", "dfq_linear_mx_q", "dfq_rms_norm_mx"):
+    for name in ("dfq_quantize_mx", "dfq_dequantize_mx", "dfq_linear_mx", "dfq_linear_mx_q", "dfq_linear_mx_variant", "dfq_rms_norm_mx"):
         getattr(L, name).restype = i32
     L.dfq_hist_shift.argtypes = [i64]
     L.dfq_hist_shift.restype = i32
@@ -467,7 +471,7 @@ def _linear_operands(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor]):
 
 
 def linear_mx(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, relu: bool = False, dtype: torch.dtype = torch.bfloat16,
-              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+              out: Optional[torch.Tensor] = None, stream=None, variant: int = LINEAR_AUTO) -> torch.Tensor:
     """x [m, k] times w [n, k] transposed, plus bias [n] float32, with relu max(., 0): [m, n] of dtype."""
     m, n, operands = _linear_operands(x, w, bias)
     code = _dtype_code(dtype)
@@ -476,16 +480,23 @@ def linear_mx(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, rel
         at, ld = out.data_ptr(), n
     else:
         at, ld = _out_rows(out, "out", dtype, m, n)
-    _check(lib().dfq_linear_mx(*operands, at, ld, code, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx")
+    if variant == LINEAR_AUTO:
+        _check(lib().dfq_linear_mx(*operands, at, ld, code, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx")
+    else:
+        _check(lib().dfq_linear_mx_variant(variant, *operands, at, ld, code, None, 0, None, 0, MX8, MX_COVER, m, n, x.k, 1 if relu else 0, _stream(stream)),
+               "dfq_linear_mx_variant")
     return out
 
 
 def linear_mx_q(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, elem: int = MX8, rule: int = MX_COVER, relu: bool = False,
-                out: Optional[MxTensor] = None, stream=None) -> MxTensor:
+                out: Optional[MxTensor] = None, stream=None, variant: int = LINEAR_AUTO) -> MxTensor:
     """The same with the result converted for the next product."""
     m, n, operands = _linear_operands(x, w, bias)
     out, q = _new_mx(m, n, elem, x.codes.device, stream) if out is None else _out_mx(out, m, n, elem)
-    _check(lib().dfq_linear_mx_q(*operands, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx_q")
+    if variant == LINEAR_AUTO:
+        _check(lib().dfq_linear_mx_q(*operands, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx_q")
+    else:
+        _check(lib().dfq_linear_mx_variant(variant, *operands, None, 0, 0, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx_variant")
     return out
 
 

@@ -35,6 +35,12 @@ __device__ __forceinline__ void load_piece_to_lds(unsigned voffset, v4i rsrc, un
                  : "memory", "m0");
 }
 
+// 4 bytes per lane straight into LDS: lane l's land at lds_base + 4 * l
+__device__ __forceinline__ void load_word_to_lds(unsigned voffset, v4i rsrc, unsigned lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voffset), "s"(rsrc), "s"(lds_base) : "memory", "m0");
+}
+
 // 16-byte store through a buffer resource: a lane whose offset is outside the buffer stores
 // nothing, so rows past the last pixel need no branch and every wavefront issues the same number
 // of stores per tile (the pacing of the load ring counts them).

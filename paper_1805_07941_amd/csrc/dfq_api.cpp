@@ -1108,17 +1108,6 @@ inline Span scales_span(const uint8_t *p, size_t lds, size_t rows, int K)
         if (tried_ != DFQ_OK) return tried_;     \
     } while (0)
 
-// the operands of a product; a.M, a.N and a.K are set
-dfq_status check_linear(const LinearMxArgs &a, dfq_mx_elem ex, dfq_mx_elem ew)
-{
-    if (!elem_ok(ex) || !elem_ok(ew)) return DFQ_EINVAL;
-    if (a.N < 1) return DFQ_ESHAPE;
-    DFQ_TRY(check_size(a.M, a.K));
-    DFQ_TRY(check_mx_rows(a.x, a.ldx, a.xs, a.ldxs, ex, a.K));
-    DFQ_TRY(check_mx_rows(a.w, a.ldw, a.ws, a.ldws, ew, a.K));
-    return (uintptr_t)a.bias % 4 ? DFQ_EINVAL : DFQ_OK;
-}
-
 }  // namespace
 
 extern "C" {
@@ -1148,36 +1137,51 @@ dfq_status dfq_dequantize_mx(const uint8_t *codes, size_t ldc, const uint8_t *sc
                                          (hipStream_t)stream));
 }
 
+dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs,
+                                 dfq_mx_elem elem_x, const uint8_t *w, size_t ldw, const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w,
+                                 const float *bias, void *y, size_t ldy, dfq_dtype dtype, uint8_t *codes, size_t ldc, uint8_t *scales,
+                                 size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream)
+{
+    const LinearMxArgs a{x, x_scales, w, w_scales, ldx, ldxs, ldw, ldws, elem_x, elem_w, bias, y, ldy, dtype,
+                         MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, M, N, K, relu ? 1 : 0};
+    if (variant < DFQ_LINEAR_AUTO || variant > DFQ_LINEAR_TILE_256X256 || !dtype_ok(dtype) || !elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
+    if (N < 1 || K < 1) return DFQ_ESHAPE;
+    if (!M) return DFQ_OK;
+    if (!elem_ok(elem_x) || !elem_ok(elem_w) || (y && codes)) return DFQ_EINVAL;
+    DFQ_TRY(check_size(M, K));
+    DFQ_TRY(check_mx_rows(x, ldx, x_scales, ldxs, elem_x, K));
+    DFQ_TRY(check_mx_rows(w, ldw, w_scales, ldws, elem_w, K));
+    if ((uintptr_t)bias % 4) return DFQ_EINVAL;
+    if (codes) {
+        DFQ_TRY(check_size(M, N));
+        DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, N));
+    } else {
+        DFQ_TRY(check_float_rows(y, ldy, dtype, N));
+    }
+    if (!apart({codes_span(x, ldx, elem_x, M, K), scales_span(x_scales, ldxs, M, K), codes_span(w, ldw, elem_w, N, K), scales_span(w_scales, ldws, N, K),
+                {bias, (size_t)N * 4}},
+               {float_span(y, ldy, dtype, M, N), codes_span(codes, ldc, elem, M, N), codes ? scales_span(scales, lds, M, N) : Span{nullptr, 0}}))
+        return DFQ_EINVAL;
+    const LinearMxForm form = (LinearMxForm)(int)variant;
+    if (form != LinearMxForm::Auto && !linear_mx_supports(a, form)) return DFQ_EUNSUPPORTED;
+    return from_hip(launch_linear_mx(a, form, (hipStream_t)stream));
+}
+
 dfq_status dfq_linear_mx(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
                          const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, void *y, size_t ldy, dfq_dtype dtype,
                          size_t M, int N, int K, int relu, dfq_stream stream)
 {
-    LinearMxArgs a{x, x_scales, w, w_scales, ldx, ldxs, ldw, ldws, elem_x, elem_w, bias, y, ldy, dtype, {}, 0, M, N, K, relu ? 1 : 0};
-    if (!dtype_ok(dtype)) return DFQ_EINVAL;
-    if (!M) return N < 1 || K < 1 ? DFQ_ESHAPE : DFQ_OK;
-    DFQ_TRY(check_linear(a, elem_x, elem_w));
-    DFQ_TRY(check_float_rows(y, ldy, dtype, N));
-    if (!apart({codes_span(x, ldx, elem_x, M, K), scales_span(x_scales, ldxs, M, K), codes_span(w, ldw, elem_w, N, K), scales_span(w_scales, ldws, N, K),
-                {bias, (size_t)N * 4}}, {float_span(y, ldy, dtype, M, N)}))
-        return DFQ_EINVAL;
-    return from_hip(launch_linear_mx(a, (hipStream_t)stream));
+    return dfq_linear_mx_variant(DFQ_LINEAR_AUTO, x, ldx, x_scales, ldxs, elem_x, w, ldw, w_scales, ldws, elem_w, bias, y, ldy, dtype, nullptr, 0, nullptr,
+                                 0, DFQ_MX8, DFQ_MX_COVER, M, N, K, relu, stream);
 }
 
 dfq_status dfq_linear_mx_q(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
                            const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, uint8_t *codes, size_t ldc,
                            uint8_t *scales, size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream)
 {
-    LinearMxArgs a{x, x_scales, w, w_scales, ldx, ldxs, ldw, ldws, elem_x, elem_w, bias, nullptr, 0, DFQ_F32,
-                   MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, M, N, K, relu ? 1 : 0};
-    if (!elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
-    if (!M) return N < 1 || K < 1 ? DFQ_ESHAPE : DFQ_OK;
-    DFQ_TRY(check_linear(a, elem_x, elem_w));
-    DFQ_TRY(check_size(M, N));
-    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, N));
-    if (!apart({codes_span(x, ldx, elem_x, M, K), scales_span(x_scales, ldxs, M, K), codes_span(w, ldw, elem_w, N, K), scales_span(w_scales, ldws, N, K),
-                {bias, (size_t)N * 4}}, {codes_span(codes, ldc, elem, M, N), scales_span(scales, lds, M, N)}))
-        return DFQ_EINVAL;
-    return from_hip(launch_linear_mx(a, (hipStream_t)stream));
+    if (M && !codes) return DFQ_EINVAL;
+    return dfq_linear_mx_variant(DFQ_LINEAR_AUTO, x, ldx, x_scales, ldxs, elem_x, w, ldw, w_scales, ldws, elem_w, bias, nullptr, 0, DFQ_F32, codes, ldc,
+                                 scales, lds, elem, rule, M, N, K, relu, stream);
 }
 
 dfq_status dfq_rms_norm_mx(const void *x, size_t ldx, const void *add, size_t ldadd, void *sum, size_t ldsum, dfq_dtype dtype,

@@ -134,10 +134,14 @@ struct LinearMxArgs {
 hipError_t launch_quantize_mx(const MxRows &x, const MxTensor &q, bool cover, hipStream_t st);
 hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t st);
 hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st);
-hipError_t launch_linear_mx(const LinearMxArgs &a, hipStream_t st);
-hipError_t launch_linear_mx_small(const LinearMxArgs &a, hipStream_t st);
-bool linear_mx_tiles_supports(const LinearMxArgs &a);
-hipError_t launch_linear_mx_tiles(const LinearMxArgs &a, hipStream_t st);
+// Which kernel a product runs (dfq_linear_mx_variant): tokens x features of a workgroup.
+enum class LinearMxForm { Auto, Direct, Stream16x16, Stream16x32, Stream32x32, Stream32x64, Tile64x64, Tile128x128, Tile256x256 };
+bool linear_mx_supports(const LinearMxArgs &a, LinearMxForm form);
+LinearMxForm linear_mx_select(const LinearMxArgs &a);
+hipError_t launch_linear_mx(const LinearMxArgs &a, LinearMxForm form, hipStream_t st);
+hipError_t launch_linear_mx_direct(const LinearMxArgs &a, hipStream_t st);
+hipError_t launch_linear_mx_stream(const LinearMxArgs &a, LinearMxForm form, hipStream_t st);
+hipError_t launch_linear_mx_tiles(const LinearMxArgs &a, LinearMxForm form, hipStream_t st);
 
 hipError_t launch_quantize(const float *x, int8_t *q, size_t n, int frac, hipStream_t st);
 hipError_t launch_quantize_i32(const float *x, int32_t *q, size_t n, int frac, hipStream_t st);

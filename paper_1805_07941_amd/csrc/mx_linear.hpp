@@ -57,8 +57,8 @@ struct Frag16 {
     __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *srow, int s, int g, int left)
     {
         const uint8_t *p = row + (size_t)s * (kWide ? 128 : 64);
-        scales = *(const unsigned *)(srow + (size_t)s * 4);
-        if (left < 4) scales &= (1u << 8 * left) - 1u;
+        scales = left > 0 ? *(const unsigned *)(srow + (size_t)s * 4) : 0u;
+        if (left < 4) scales &= (1u << 8 * max(left, 0)) - 1u;
         const v4i none = {0, 0, 0, 0};
         if constexpr (kWide) {
             lo = (g >> 1) < left ? *(const v4i *)(p + 16 * g) : none;
@@ -73,6 +73,22 @@ struct Frag16 {
         }
         if constexpr (!EXACT) scales >>= 8 * g;
         else scales >>= 8 * (g >> 1);
+    }
+    // the same from a row in LDS whose pieces are XOR-ed with `key`; step j of the row, scales at srow
+    __device__ __forceinline__ void read(const char *row, int key, const char *srow, int j, int g, int left)
+    {
+        typedef int v2i __attribute__((ext_vector_type(2)));
+        if constexpr (kWide) {
+            lo = *(const v4i *)(row + (((8 * j + g) ^ key) * 16));
+            hi = *(const v4i *)(row + (((8 * j + 4 + g) ^ key) * 16));
+        } else if constexpr (EXACT) {
+            const v2i a = *(const v2i *)(row + (((4 * j + (g >> 1)) ^ key) * 16) + 8 * (g & 1)), b = *(const v2i *)(row + (((4 * j + 2 + (g >> 1)) ^ key) * 16) + 8 * (g & 1));
+            lo = v4i{a[0], a[1], b[0], b[1]};
+        } else {
+            lo = *(const v4i *)(row + (((4 * j + g) ^ key) * 16));
+        }
+        scales = *(const unsigned *)(srow + 4 * j) & (left >= 4 ? ~0u : (1u << 8 * max(left, 0)) - 1u);
+        scales >>= EXACT ? 8 * (g >> 1) : 8 * g;
     }
     __device__ __forceinline__ v8i codes() const
     {

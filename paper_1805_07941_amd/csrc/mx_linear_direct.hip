@@ -1,6 +1,7 @@
 // The inner product on microscaled operands, y[m][n] = sum_k x[m][k] * w[n][k], without staging: a wavefront reads its operands from
 // global memory straight into the registers of the matrix instruction, the wavefronts of a workgroup share the reduction axis and
-// their sums meet in LDS in a fixed order.
+// their sums meet in LDS in a fixed order.  64-bit addresses throughout: for rows further apart than the other kernels' 31-bit
+// offsets reach.
 //
 // v_mfma_scale_f32_16x16x128_f8f6f4: rows of the first operand are features, columns of the second tokens; lane l holds row l % 16
 // and, with g = l / 16, of 4-bit elements the block g of the step's four (16 bytes), of 8-bit ones bytes 16g..16g+15 of the step's
@@ -14,8 +15,8 @@ namespace {
 
 // EXACT: the elements times their scales as bfloat16 (they fit its significand) on the bfloat16 matrix instructions, whose products
 // and sums keep float32's accuracy; see launch_linear_mx.
-template <int EX, int EW, bool EXACT, int FT, int TT, int NW>
-__global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a)
+template <int EX, int EW, bool EXACT, int FT, int TT, int NW, int U>
+__global__ void __launch_bounds__(NW * 64) linear_mx_direct_kernel(LinearMxArgs a)
 {
     constexpr int F = FT * 16, T = TT * 16;
     constexpr int kPad = F + 4;                          // floats between tokens of the partial sums
@@ -50,23 +51,30 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a
 #pragma unroll
         for (int t = 0; t < TT; t++) acc[f][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
-    auto step = [&](int s, auto tail) __attribute__((always_inline)) {
-        Frag16<EW, EXACT> fw[FT];
-        Frag16<EX, EXACT> fx[TT];
-        const int left = decltype(tail)::value ? nb - s * 4 : 4;       // blocks of this step
+    // U steps at a time, so that their loads are in flight together; the wavefront's last ones, among them a last step of fewer than
+    // four blocks, as one group whose missing blocks are zeros
+    auto group = [&](int s, int end, auto whole) __attribute__((always_inline)) {
+        Frag16<EW, EXACT> fw[U][FT];
+        Frag16<EX, EXACT> fx[U][TT];
 #pragma unroll
-        for (int f = 0; f < FT; f++) fw[f].load(wp[f], wsp[f], s, g, left);
+        for (int u = 0; u < U; u++) {
+            const int left = decltype(whole)::value ? 4 : s + u < end ? min(nb - (s + u) * 4, 4) : 0;
 #pragma unroll
-        for (int t = 0; t < TT; t++) fx[t].load(xp[t], xsp[t], s, g, left);
+            for (int f = 0; f < FT; f++) fw[u][f].load(wp[f], wsp[f], s + u, g, left);
 #pragma unroll
-        for (int f = 0; f < FT; f++)
+            for (int t = 0; t < TT; t++) fx[u][t].load(xp[t], xsp[t], s + u, g, left);
+        }
 #pragma unroll
-            for (int t = 0; t < TT; t++) acc[f][t] = multiply16(fw[f], fx[t], acc[f][t]);
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int f = 0; f < FT; f++)
+#pragma unroll
+                for (int t = 0; t < TT; t++) acc[f][t] = multiply16(fw[u][f], fx[u][t], acc[f][t]);
     };
-    const int per = (steps + NW - 1) / NW, s1 = min(steps, (wave + 1) * per), full = min(s1, nb / 4);
+    const int per = (steps + NW - 1) / NW, s1 = min(steps, (wave + 1) * per), whole = min(s1, nb / 4);
     int s = wave * per;
-    for (; s < full; s++) step(s, std::false_type{});
-    for (; s < s1; s++) step(s, std::true_type{});
+    for (; s + U <= whole; s += U) group(s, s1, std::true_type{});
+    for (; s < s1; s += U) group(s, s1, std::false_type{});
 
     // lane: features 4g .. 4g+3 of token l16 of each tile
 #pragma unroll
@@ -80,7 +88,7 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a
         const int t = i / kOctets, o = i % kOctets;
         const size_t m = m0 + t;
         float v[8] = {};
-#pragma unroll
+#pragma unroll 2
         for (int w = 0; w < NW; w++) {
             const v4f *p = (const v4f *)&part[w][t][o * 8];
 #pragma unroll
@@ -93,17 +101,16 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_small_kernel(LinearMxArgs a
     }
 }
 
-template <int EX, int EW, bool EXACT>
+template <int EX, int EW, bool EXACT, int FT, int TT, int NW, int U>
 hipError_t run(const LinearMxArgs &a, hipStream_t st)
 {
-    constexpr int FT = 2, TT = 1, NW = 4;
     const size_t most = 65535;                           // rows of the grid
     for (size_t m = 0; m < a.M; m += most * TT * 16) {
         LinearMxArgs b = a;
         advance_tokens(b, m);
         b.M = a.M - m < most * TT * 16 ? a.M - m : most * TT * 16;
         const dim3 grid((unsigned)((a.N + FT * 16 - 1) / (FT * 16)), (unsigned)((b.M + TT * 16 - 1) / (TT * 16)));
-        linear_mx_small_kernel<EX, EW, EXACT, FT, TT, NW><<<grid, NW * 64, 0, st>>>(b);
+        linear_mx_direct_kernel<EX, EW, EXACT, FT, TT, NW, U><<<grid, NW * 64, 0, st>>>(b);
     }
     return hipGetLastError();
 }
@@ -112,22 +119,16 @@ template <int EX, int EW>
 hipError_t by_output(const LinearMxArgs &a, hipStream_t st)
 {
     if constexpr (EX == kMx8 || EW == kMx8)
-        if (!a.q.codes && a.dtype == kF32) return run<EX, EW, true>(a, st);
-    return run<EX, EW, false>(a, st);
+        if (!a.q.codes && a.dtype == kF32) return run<EX, EW, true, 2, 1, 4, 2>(a, st);
+    return run<EX, EW, false, 2, 1, 4, 2>(a, st);
 }
 
 }  // namespace
 
-hipError_t launch_linear_mx_small(const LinearMxArgs &a, hipStream_t st)
+hipError_t launch_linear_mx_direct(const LinearMxArgs &a, hipStream_t st)
 {
     if (a.elem_x == kMx4) return a.elem_w == kMx4 ? by_output<kMx4, kMx4>(a, st) : by_output<kMx4, kMx8>(a, st);
     return a.elem_w == kMx4 ? by_output<kMx8, kMx4>(a, st) : by_output<kMx8, kMx8>(a, st);
-}
-
-hipError_t launch_linear_mx(const LinearMxArgs &a, hipStream_t st)
-{
-    if (a.M > 128 && linear_mx_tiles_supports(a)) return launch_linear_mx_tiles(a, st);
-    return launch_linear_mx_small(a, st);
 }
 
 }  // namespace dfq

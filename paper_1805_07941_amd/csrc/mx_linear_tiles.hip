@@ -2,13 +2,12 @@
 //
 // acc[n][m] = sum_k w[n][k] * x[m][k]: features are the rows of the matrix instruction's first operand and tokens the columns of its
 // second; feature rows lie in LDS in an order that leaves 16 consecutive features of one token in each lane.  A workgroup walks the
-// reduction axis in steps of 128 bytes of an operand row (256 values of 4 bits, 128 where an operand has 8) through two LDS stages
-// that direct global -> LDS loads fill, one barrier to a step.  A wavefront waits for its own loads of the step it is about to
+// reduction axis in steps of 128 bytes of an operand row (256 values of 4 bits, 128 where an operand has 8) through a ring of LDS
+// stages that direct global -> LDS loads fill, one barrier to a step.  A wavefront waits for its own loads of the step it is about to
 // read only, and reads the next 64 values' operands while the matrix pipe is busy with these.
 //
 // Scales come in chunks of 16 bytes of a row (512 values): a row's four bytes of one step would cost as many cache lines as its 128
-// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c; three buffers, because loads run two steps ahead of
-// the reads.  What lies behind a row's last block is masked twice: codes by an offset past the buffer (zeros arrive), scales by a
+// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c, into a ring of its own.  What lies behind a row's last block is masked twice: codes by an offset past the buffer (zeros arrive), scales by a
 // comparison when they are read, so that neither the next row's bytes nor padding count.
 #include "conv_ring.hpp"
 #include "mx_linear.hpp"
@@ -25,12 +24,6 @@ struct TileParams {
     int steps;
     int tiles_m, tiles_n;
 };
-
-// 4 bytes per lane straight into LDS: lane l's land at lds_base + 4 * l
-__device__ __forceinline__ void load_word_to_lds(unsigned voffset, v4i rsrc, unsigned lds_base)
-{
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voffset), "s"(rsrc), "s"(lds_base) : "memory", "m0");
-}
 
 // f(0), f(1), .. f(N - 1) with the number as a type
 template <int N, int I = 0, class F>
@@ -51,6 +44,9 @@ struct Operand {
     __device__ static __forceinline__ int place(int row, int piece) { return kRow == 128 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3); }
 };
 
+// chunks of scales in LDS: chunk s / SPC + 1 is loaded with step s, up to NST steps ahead of the one that is read
+constexpr int scale_chunks(int nst, int spc) { return (nst + spc - 1) / spc + 2; }
+
 // where a row's words of a chunk of scales are
 __device__ __forceinline__ int scale_key(int row) { return (row >> 3) & 3; }
 
@@ -63,8 +59,8 @@ struct Frag32 {
     unsigned scale, scale1;
 };
 
-template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_kernel(TileParams prm)
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST>
+__global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(TileParams prm)
 {
     constexpr int NW = WM * WN;
     constexpr int KS = EX == kMx4 && EW == kMx4 ? 256 : 128;
@@ -74,14 +70,15 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int XL = BM * OX::kRow / 1024 / NW, WL = BN * OW::kRow / 1024 / NW;     // code loads of a wavefront in a step
     constexpr int SPC = 512 / KS;                                      // steps of a chunk of scales
-    constexpr int SL = (BM + BN) / 16 / SPC / NW;                      // scale loads of a wavefront in a step
-    static_assert(XL * NW * 1024 == BM * OX::kRow && WL * NW * 1024 == BN * OW::kRow && SL * SPC * NW * 16 == BM + BN, "whole loads");
+    constexpr int SL = ((BM + BN) / 16 + SPC * NW - 1) / (SPC * NW);   // scale loads of a wavefront in a step
+    static_assert(XL * NW * 1024 == BM * OX::kRow && WL * NW * 1024 == BN * OW::kRow, "whole loads");
     constexpr int LPS = XL + WL + SL;
-    static_assert(SPC * SL + 2 * LPS < 64, "outstanding loads fit the counter");
+    static_assert(NST >= 2 && SPC * SL + NST * LPS < 64, "outstanding loads fit the counter");
+    constexpr int NCH = scale_chunks(NST, SPC);
     constexpr int kStage = BM * OX::kRow + BN * OW::kRow;
-    constexpr int kChunk = (BM + BN) * 16;
+    constexpr int kChunk = SL * SPC * NW * 256;                        // (rows past the tile's: loads to keep their number even)
 
-    extern __shared__ char lds[];                                      // two stages, then three chunks of scales
+    extern __shared__ char lds[];                                      // NST stages, then NCH chunks of scales
     const LinearMxArgs &a = prm.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h = lane >> 5;
@@ -129,7 +126,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // load j of a chunk
     auto issue_scales = [&](int j, int chunk) __attribute__((always_inline)) {
         const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane(
-            (int)(lds_base + 2 * kStage + (unsigned)(chunk % 3) * kChunk + (unsigned)(wave + NW * j) * 256u));
+            (int)(lds_base + NST * kStage + (unsigned)(chunk % NCH) * kChunk + (unsigned)(wave + NW * j) * 256u));
         const bool x = j < BM / (16 * NW);
         const v4i r = {x ? xsr.x : wsr.x, x ? xsr.y : wsr.y, x ? xsr.z : wsr.z, wsr.w};
         const unsigned moved = x ? (unsigned)j * (16 * NW) * ldxs : (unsigned)(j - BM / (16 * NW)) * (16 * NW) * ldws;
@@ -169,7 +166,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     const unsigned xlane = (unsigned)(wm0 + l32) * OX::kRow, wlane = (unsigned)(BM * OX::kRow + (wn0 + l32) * OW::kRow);
     const unsigned xkey = OX::place(l32, 0) * 16, wkey = OW::place(l32, 0) * 16;
     const unsigned skey = scale_key(l32) * 4;
-    const unsigned xslane = (unsigned)(2 * kStage + (wm0 + l32) * 16), wslane = (unsigned)(2 * kStage + (BM + wn0 + l32) * 16);
+    const unsigned xslane = (unsigned)(NST * kStage + (wm0 + l32) * 16), wslane = (unsigned)(NST * kStage + (BM + wn0 + l32) * 16);
     auto read_rows = [&](auto &f, auto op, unsigned at, unsigned key, unsigned scale_at, int kk, unsigned b0, unsigned b1) __attribute__((always_inline)) {
         constexpr bool wide = decltype(op)::kRow * 8 / KS == 8;
         if constexpr (wide) {
@@ -195,7 +192,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     };
     auto part_of = [&](int step, int stage, int kk) __attribute__((always_inline)) {
         const int block = (step * KK + kk) * 2;                        // the first of the two
-        return Part{kk, (unsigned)stage * kStage, (unsigned)(step / SPC % 3 * kChunk) + ((unsigned)(block & 12) ^ skey) + (unsigned)(block & 2),
+        return Part{kk, (unsigned)stage * kStage, (unsigned)(step / SPC % NCH * kChunk) + ((unsigned)(block & 12) ^ skey) + (unsigned)(block & 2),
                     block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, block + 1 < prm.nb ? 255u : 0u};
     };
     auto read_w = [&](Frag32<EW, EXACT> &f, int n, const Part &p) __attribute__((always_inline)) {
@@ -236,9 +233,10 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     const int steps = prm.steps;
 #pragma unroll
     for (int j = 0; j < SPC * SL; j++) issue_scales(j, 0);
-    issue(0, 0, None{}, std::integral_constant<int, LPS>{});
-    issue(1, 1, None{}, std::integral_constant<int, kFirst>{});
-    wait_loads<kFirst>();
+#pragma unroll
+    for (int i = 0; i < NST - 1; i++) issue(i, i, None{}, std::integral_constant<int, LPS>{});
+    issue(NST - 1, NST - 1, None{}, std::integral_constant<int, kFirst>{});
+    wait_loads<(NST - 2) * LPS + kFirst>();
     ring_barrier();
     {
         const Part p = part_of(0, 0, 0);
@@ -253,7 +251,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // wavefronts meet there, the next step having arrived, and the stage is filled again.  Steps past the last are all out of range:
     // their loads bring zeros, touch no memory, and keep one form of the loop.
     for (int i = 0, stage = 0; i < steps; i++) {
-        const int next = stage ^ 1;
+        const int next = stage + 1 == NST ? 0 : stage + 1, last = stage == 0 ? NST - 1 : stage - 1;
         static_for<KK>([&](auto part) __attribute__((always_inline)) {
             constexpr int kk = decltype(part)::value;
             const Part p = kk + 1 < KK ? part_of(i, stage, kk + 1) : part_of(i + 1, next, 0);
@@ -263,7 +261,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (m == 0) {
                     if constexpr (kk == KK - 1) {
-                        wait_loads<0>();
+                        wait_loads<(NST - 2) * LPS>();
                         ring_barrier();
                     }
 #pragma unroll
@@ -271,8 +269,8 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
                 }
                 read_x(m, p);
                 constexpr int late = TM == 1 ? m : m - 1;
-                if constexpr (kk == KK - 1 && late >= 0 && late < kLate) issue_slot(i + 2, stage, std::integral_constant<int, late < 0 ? 0 : late>{});
-                if constexpr (kk == 0 && kSlots > kLate) issue_slot(i + 1, next, std::integral_constant<int, kLate + m>{});
+                if constexpr (kk == KK - 1 && late >= 0 && late < kLate) issue_slot(i + NST, stage, std::integral_constant<int, late < 0 ? 0 : late>{});
+                if constexpr (kk == 0 && kSlots > kLate) issue_slot(i + NST - 1, last, std::integral_constant<int, kLate + m>{});
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
@@ -283,7 +281,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     // ---- results: lane holds features wn0 + 32n + 16h + 0..15 of token wm0 + 32m + l32.  32 tokens at a time go through the
     // wavefront's own part of LDS, so that a row's features leave in whole cache lines, an octet to a lane.
     constexpr int F = TN * 32, kPad = F + 4;
-    static_assert(NW * 32 * kPad * 4 <= 2 * kStage + 3 * kChunk, "LDS for the results");
+    static_assert(NW * 32 * kPad * 4 <= NST * kStage + NCH * kChunk, "LDS for the results");
     __syncthreads();                                                   // every wavefront has read its last operands
     float *mine = (float *)lds + wave * 32 * kPad;
     constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
@@ -316,13 +314,14 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN / 4) linear_mx_tiles_ker
     }
 }
 
-template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN>
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST>
 hipError_t run(const LinearMxArgs &a, hipStream_t st)
 {
     constexpr int KS = EX == kMx4 && EW == kMx4 ? 256 : 128;
-    constexpr int kLds = 2 * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + 3 * (BM + BN) * 16;
+    constexpr int kParts = 512 / KS * WM * WN;                         // loads of scales come in multiples of this
+    constexpr int kLds = NST * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + scale_chunks(NST, 512 / KS) * (((BM + BN) / 16 + kParts - 1) / kParts * kParts * 256);
     static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
-    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN>;
+    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN, OCC, NST>;
     static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (allowed != hipSuccess) return allowed;
     TileParams p{a, (a.K + kMxBlock - 1) / kMxBlock};
@@ -341,27 +340,25 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
 }
 
 template <int EX, int EW, bool EXACT>
-hipError_t by_shape(const LinearMxArgs &a, hipStream_t st)
+hipError_t by_shape(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 {
-    return run<EX, EW, EXACT, 256, 256, 2, 4>(a, st);
+    switch (form) {
+        case LinearMxForm::Tile64x64: return run<EX, EW, EXACT, 64, 64, 2, 2, 3, 3>(a, st);
+        case LinearMxForm::Tile128x128: return run<EX, EW, EXACT, 128, 128, 2, 2, 2, 2>(a, st);
+        case LinearMxForm::Tile256x256: return run<EX, EW, EXACT, 256, 256, 2, 4, 2, 2>(a, st);
+        default: return hipErrorInvalidValue;
+    }
 }
 
 }  // namespace
 
-bool linear_mx_tiles_supports(const LinearMxArgs &a)
-{
-    // offsets inside a tile of 256 rows have 31 bits
-    constexpr size_t most = (size_t)1 << 22;
-    return a.ldx <= most && a.ldw <= most && a.ldxs <= most && a.ldws <= most;
-}
-
-hipError_t launch_linear_mx_tiles(const LinearMxArgs &a, hipStream_t st)
+hipError_t launch_linear_mx_tiles(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 {
     const bool exact = !a.q.codes && a.dtype == kF32;
-    if (a.elem_x == kMx4 && a.elem_w == kMx4) return by_shape<kMx4, kMx4, false>(a, st);
-    if (a.elem_x == kMx4) return exact ? by_shape<kMx4, kMx8, true>(a, st) : by_shape<kMx4, kMx8, false>(a, st);
-    if (a.elem_w == kMx4) return exact ? by_shape<kMx8, kMx4, true>(a, st) : by_shape<kMx8, kMx4, false>(a, st);
-    return exact ? by_shape<kMx8, kMx8, true>(a, st) : by_shape<kMx8, kMx8, false>(a, st);
+    if (a.elem_x == kMx4 && a.elem_w == kMx4) return by_shape<kMx4, kMx4, false>(a, form, st);
+    if (a.elem_x == kMx4) return exact ? by_shape<kMx4, kMx8, true>(a, form, st) : by_shape<kMx4, kMx8, false>(a, form, st);
+    if (a.elem_w == kMx4) return exact ? by_shape<kMx8, kMx4, true>(a, form, st) : by_shape<kMx8, kMx4, false>(a, form, st);
+    return exact ? by_shape<kMx8, kMx8, true>(a, form, st) : by_shape<kMx8, kMx8, false>(a, form, st);
 }
 
 }  // namespace dfq

@@ -1,5 +1,6 @@
 """GPU parity of the microscaled operators with their oracle: conversions byte for byte, products and norms within bounds that follow from
 float32's step u = 2^-24, from what the matrix instructions keep (csrc/mx_linear.hpp) and from half a step of the result's type."""
+import functools
 import zlib
 
 import numpy as np
@@ -162,12 +163,9 @@ def product_bound(x, w, bias, elems, exact):
     total = np.abs(x) @ np.abs(w).T + (0 if bias is None else np.abs(bias))
     err = (K + 8) * U * total
     if not exact and 8 in elems:
-        pad = -K % 8
-        big = np.zeros(total.shape)
-        xp, wp = np.pad(np.abs(x), ((0, 0), (0, pad))), np.pad(np.abs(w), ((0, 0), (0, pad)))
-        for k in range(0, K, 8):
-            big += (xp[:, None, k:k + 8] * wp[None, :, k:k + 8]).max(2)
-        err = err + 7 * 2.0 ** -13 * big
+        xp, wp = (torch.nn.functional.pad(torch.from_numpy(np.abs(v)).to(DEV), (0, -K % 8)) for v in (x, w))
+        big = sum((xp[:, None, k:k + 8] * wp[None, :, k:k + 8]).amax(2) for k in range(0, K, 8))
+        err = err + 7 * 2.0 ** -13 * big.cpu().numpy()
     return err
 
 
@@ -188,11 +186,12 @@ SHAPES = [(1, 1, 1), (1, 16, 32), (2, 33, 40), (1, 64, 129), (16, 48, 512), (17,
 def test_linear(B, ex, ew, M, N, K):
     rng = rng_of(ex, ew, M, N, K)
     (x, w, b), (vx, vw, vb) = products(B, rng, M, N, K, ex, ew, M % 2 == 1)
+    bounds = [product_bound(vx, vw, vb, (ex, ew), exact) for exact in (False, True)]
     for relu in (False, True):
         want = mx.linear(vx, vw, vb, relu)
         for out in TYPES:
             y = host(B.linear_mx(x, w, b, relu, TYPES[out]))
-            tol = product_bound(vx, vw, vb, (ex, ew), out == "f32")
+            tol = bounds[out == "f32"]
             tol = tol + HALF[out] * (np.abs(want) + tol) + (2.0 ** -25 if out == "f16" else 0)
             ok = np.abs(y - want) <= tol
             ok |= np.isinf(y) & (np.abs(want) + tol > 65504) if out == "f16" else False
@@ -212,9 +211,10 @@ def steps_of(v, scale, elem):
 def test_linear_q(B, ex, ew, elem, M, N, K):
     rng = rng_of(ex, ew, elem, M, N, K)
     (x, w, b), (vx, vw, vb) = products(B, rng, M, N, K, ex, ew, N % 2 == 0)
+    err = product_bound(vx, vw, vb, (ex, ew), False)
     for rule, relu in ((mx.COVER, True), (mx.FLOOR, False)):
         q = B.linear_mx_q(x, w, b, ELEM[elem], rule, relu)
-        want, err = mx.linear(vx, vw, vb, relu), product_bound(vx, vw, vb, (ex, ew), False)
+        want = mx.linear(vx, vw, vb, relu)
         codes, scales = host(q.codes), host(q.scales)
         nb = -(-N // 32)
         assert not scales[:, nb:].any()
@@ -234,6 +234,55 @@ def test_linear_q(B, ex, ew, elem, M, N, K):
         half = np.maximum(steps_of(np.abs(near) + ewide, scale, elem), steps_of(near, scale, elem))
         ok = np.abs(got - near) <= ewide + half
         assert ok.all(), (np.argwhere(~ok)[:4], rule)
+
+
+VARIANT_SHAPES = [(1, 1, 1), (3, 35, 97), (16, 32, 300), (33, 65, 513), (70, 100, 1025), (130, 140, 1600), (257, 300, 700)]
+
+
+@functools.lru_cache(maxsize=None)
+def variant_case(B, ex, ew, M, N, K):
+    gpu, (vx, vw, vb) = products(B, rng_of("variant", ex, ew, M, N, K), M, N, K, ex, ew, True)
+    return gpu, mx.linear(vx, vw, vb, True), [product_bound(vx, vw, vb, (ex, ew), exact) for exact in (False, True)]
+
+
+@pytest.mark.parametrize("variant", range(1, 9))
+@pytest.mark.parametrize("ex, ew", PAIRS)
+def test_linear_by_every_kernel(B, ex, ew, variant):
+    """Each kernel on the same calls, tiles of every kind of edge among them: within the bounds, and converted as its own float32 values
+    would be (4-bit operands: the same products in every kernel)."""
+    for M, N, K in VARIANT_SHAPES:
+        (x, w, b), want, bounds = variant_case(B, ex, ew, M, N, K)
+        for out in TYPES:
+            y = host(B.linear_mx(x, w, b, True, TYPES[out], variant=variant))
+            tol = bounds[out == "f32"]
+            tol = tol + HALF[out] * (want + tol) + (2.0 ** -25 if out == "f16" else 0)
+            ok = (np.abs(y - want) <= tol) | ((out == "f16") & np.isinf(y) & (want + tol > 65504))
+            assert ok.all(), (M, N, K, out, np.argwhere(~ok)[:4])
+        if variant == 2:                                     # half of a block to a workgroup
+            with pytest.raises(B.DfqError):
+                B.linear_mx_q(x, w, b, variant=variant)
+        else:
+            q = B.linear_mx_q(x, w, b, B.MX8, relu=True, variant=variant)
+            if ex == ew == 4:
+                assert torch.equal(q.codes, B.quantize_mx(B.linear_mx(x, w, b, True, torch.float32, variant=variant)).codes)
+            off = np.abs(host(B.dequantize_mx(q)) - want)
+            blocks = np.pad(want, ((0, 0), (0, -N % 32))).reshape(M, -1, 32).max(2).repeat(32, 1)[:, :N]
+            assert (off <= bounds[0] * (1 + 2.0 ** -3) + np.maximum(2.0 ** -4 * want, 2.0 ** -17 * blocks)).all()
+
+
+def test_linear_rows_too_far_apart_for_tiles(B):
+    """Rows of an operand beyond the reach of 31-bit offsets: by 64-bit addresses, the same sums."""
+    rng = rng_of("reach")
+    M, N, K, ld = 5, 40, 96, (1 << 22) + 16
+    (x, w, b), (vx, vw, vb) = products(B, rng, M, N, K, 8, 4, True)
+    room = torch.full((M * ld,), 0x7f, dtype=torch.uint8, device=DEV)
+    codes = room.as_strided((M, 96), (ld, 1))
+    codes.copy_(x.codes)
+    far = B.MxTensor(codes, x.scales, x.elem, K)
+    want = mx.linear(vx, vw, vb)
+    assert (np.abs(host(B.linear_mx(far, w, b, dtype=torch.float32)) - want) <= product_bound(vx, vw, vb, (8, 4), True) + U * np.abs(want)).all()
+    with pytest.raises(B.DfqError):
+        B.linear_mx(far, w, b, variant=8)
 
 
 def test_linear_keeps_what_is_no_number(B):

@@ -85,6 +85,20 @@ def test_linear_q_refuses(kw, status):
     assert linear_q(**kw) == status
 
 
+def variant(which, **kw):
+    a = dict(OPERANDS, y=A[4], ldy=16, dtype=1, codes=None, ldc=0, scales=None, lds=0, elem=B.MX8, rule=0, M=3, N=16, K=64, relu=0)
+    a.update(kw)
+    return B.lib().dfq_linear_mx_variant(which, *a.values(), None)
+
+
+@pytest.mark.parametrize("which, kw, status", [
+    (-1, {}, B.EINVAL), (9, {}, B.EINVAL), (3, dict(codes=A[5], ldc=32, scales=A[6], lds=4), B.EINVAL), (3, dict(y=None), B.EINVAL), (8, dict(ldy=15), B.ESHAPE),
+    (2, dict(y=None, codes=A[5], ldc=32, scales=A[6], lds=4), B.EUNSUPPORTED), (8, dict(ldx=(1 << 22) + 16), B.EUNSUPPORTED),
+    (3, dict(ldws=(1 << 22) + 4), B.EUNSUPPORTED), (0, dict(y=None, codes=A[5], ldc=16, scales=A[6], lds=4), B.ESHAPE)])
+def test_linear_variant_refuses(which, kw, status):
+    assert variant(which, **kw) == status
+
+
 @pytest.mark.parametrize("kw, status", [
     (dict(x=None), B.EINVAL), (dict(y=None, codes=None), B.EINVAL), (dict(scales=None), B.EINVAL), (dict(dtype=3), B.EINVAL), (dict(wtype=2), B.EINVAL),
     (dict(eps=-1.0), B.EINVAL), (dict(eps=float("nan")), B.EINVAL), (dict(eps=float("inf")), B.EINVAL), (dict(K=0), B.ESHAPE), (dict(ldadd=60), B.ESHAPE),
