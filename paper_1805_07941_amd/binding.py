@@ -10,7 +10,6 @@ import ctypes as C
 import os
 import struct
 from array import array
-from contextlib import nullcontext
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -343,11 +342,13 @@ class MxTensor(NamedTuple):
     @classmethod
     def empty(cls, rows: int, k: int, elem: int, device="cuda") -> "MxTensor":
         nb = (k + 31) >> 5
-        return cls(torch.empty((rows, nb << 5 if elem == MX8 else nb << 4), dtype=torch.uint8, device=device),
-                   torch.empty((rows, nb + 3 & -4), dtype=torch.uint8, device=device), elem, k)
+        return cls(_empty(rows, nb << 5 if elem == MX8 else nb << 4, dtype=_U8, device=device), _empty(rows, nb + 3 & -4, dtype=_U8, device=device), elem, k)
 
 
-# (What these check is read once: a call on one token is bound by the host.)
+# (A call on one token is bound by the host: what these check is read once.)
+_U8, _empty = torch.uint8, torch.empty
+
+
 def _here(t: torch.Tensor, name: str):
     """A launch goes to the current device."""
     at = t.get_device()
@@ -355,11 +356,14 @@ def _here(t: torch.Tensor, name: str):
         raise ValueError(f"{name}: expected a tensor on the current CUDA device")
 
 
+def _stream_here(stream) -> int:
+    """_stream() where a tensor is known to be on the current device."""
+    return _raw_stream(_current_device()) if stream is None and _raw_stream is not None else _stream(stream)
+
+
 def _rows(t: torch.Tensor, name: str, dtype=None):
     """(address, row distance, rows, k) of [rows, k] with whole rows, or of a contiguous tensor of more dimensions as its rows."""
-    at = t.get_device()
-    if at < 0 or at != _current_device():
-        raise ValueError(f"{name}: expected a tensor on the current CUDA device")
+    _here(t, name)
     if (t.dtype is not dtype) if dtype is not None else t.dtype not in MX_DTYPES:
         raise TypeError(f"{name}: expected {dtype or 'float32, bfloat16 or float16'}")
     shape = t.shape
@@ -382,18 +386,31 @@ def _rows(t: torch.Tensor, name: str, dtype=None):
 def _mx(q: MxTensor, name: str, rows: Optional[int] = None, k: Optional[int] = None):
     """Checks a microscaled tensor; returns (codes, their row distance, scales, their row distance) and its number of rows."""
     codes, scales, elem, n = q
-    if codes.dim() != 2 or scales.dim() != 2:
+    at = codes.get_device()
+    if at < 0 or scales.get_device() != at or at != _current_device():
+        raise ValueError(f"{name}: expected tensors on the current CUDA device")
+    if codes.dtype is not _U8 or scales.dtype is not _U8:
+        raise TypeError(f"{name}: expected torch.uint8")
+    shape, sshape = codes.shape, scales.shape
+    if len(shape) != 2 or len(sshape) != 2:
         raise ValueError(f"{name}: expected [rows, bytes]")
-    c, ldc, have, width = _rows(codes, name, torch.uint8)
-    s, lds, srows, swidth = _rows(scales, name, torch.uint8)
+    have, width = shape
+    ldc, step = codes.stride()
+    lds, sstep = scales.stride()
     if elem not in (MX4, MX8) or n < 1:
         raise ValueError(f"{name}: no such element, or no values")
     nb = (n + 31) >> 5
-    if have != srows or width < (nb << 5 if elem == MX8 else nb << 4) or swidth < nb + 3 & -4:
+    if have != sshape[0] or width < (nb << 5 if elem == MX8 else nb << 4) or sshape[1] < nb + 3 & -4:
         raise ValueError(f"{name}: codes and scales do not hold rows of {n} values")
+    if step != 1 or sstep != 1:
+        raise ValueError(f"{name}: the bytes of a row have to be next to each other")
+    if have <= 1:
+        ldc, lds = nb << 5, nb + 3 & -4
+    elif ldc < width or lds < sshape[1]:
+        raise ValueError(f"{name}: rows overlap")
     if (rows is not None and have != rows) or (k is not None and n != k):
         raise ValueError(f"{name}: expected {have if rows is None else rows} rows of {n if k is None else k} values")
-    return (c, ldc, s, lds), have
+    return (codes.data_ptr(), ldc, scales.data_ptr(), lds), have
 
 
 def _allocating_on(stream):
@@ -403,20 +420,25 @@ def _allocating_on(stream):
 
 def _new(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty(*shape, dtype=dtype, device=device)
     with _allocating_on(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty(*shape, dtype=dtype, device=device)
+
+
+def _like(t: torch.Tensor, stream) -> torch.Tensor:
+    """A dense tensor of t's shape and type."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with _allocating_on(stream):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _new_mx(rows: int, k: int, elem: int, device, stream):
     """A fresh microscaled tensor, and what _mx gives for it."""
-    if stream is None:
-        q = MxTensor.empty(rows, k, elem, device)
-    else:
-        with _allocating_on(stream):
-            q = MxTensor.empty(rows, k, elem, device)
     nb = (k + 31) >> 5
-    return q, (q.codes.data_ptr(), nb << 5 if elem == MX8 else nb << 4, q.scales.data_ptr(), nb + 3 & -4)
+    width, swidth = nb << 5 if elem == MX8 else nb << 4, nb + 3 & -4
+    codes, scales = _new((rows, width), _U8, device, stream), _new((rows, swidth), _U8, device, stream)
+    return MxTensor(codes, scales, elem, k), (codes.data_ptr(), width, scales.data_ptr(), swidth)
 
 
 def _out_mx(out: MxTensor, rows: int, k: int, elem: int):
@@ -443,7 +465,7 @@ def quantize_mx(x: torch.Tensor, elem: int = MX8, rule: int = MX_COVER, out: Opt
     """float32, bfloat16 or float16 rows -> microscaled ones; the rows of a tensor of more dimensions are its last one's."""
     at, ld, rows, k = _rows(x, "x")
     out, q = _new_mx(rows, k, elem, x.device, stream) if out is None else _out_mx(out, rows, k, elem)
-    _check(lib().dfq_quantize_mx(at, ld, MX_DTYPES[x.dtype], rows, k, *q, elem, rule, _stream(stream)), "dfq_quantize_mx")
+    _check(lib().dfq_quantize_mx(at, ld, MX_DTYPES[x.dtype], rows, k, *q, elem, rule, _stream_here(stream)), "dfq_quantize_mx")
     return out
 
 
@@ -456,7 +478,7 @@ def dequantize_mx(q: MxTensor, dtype: torch.dtype = torch.float32, out: Optional
         at, ld = out.data_ptr(), k
     else:
         at, ld = _out_rows(out, "out", dtype, rows, k)
-    _check(lib().dfq_dequantize_mx(*held, q.elem, rows, k, at, ld, code, _stream(stream)), "dfq_dequantize_mx")
+    _check(lib().dfq_dequantize_mx(*held, q.elem, rows, k, at, ld, code, _stream_here(stream)), "dfq_dequantize_mx")
     return out
 
 
@@ -481,9 +503,9 @@ def linear_mx(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, rel
     else:
         at, ld = _out_rows(out, "out", dtype, m, n)
     if variant == LINEAR_AUTO:
-        _check(lib().dfq_linear_mx(*operands, at, ld, code, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx")
+        _check(lib().dfq_linear_mx(*operands, at, ld, code, m, n, x.k, 1 if relu else 0, _stream_here(stream)), "dfq_linear_mx")
     else:
-        _check(lib().dfq_linear_mx_variant(variant, *operands, at, ld, code, None, 0, None, 0, MX8, MX_COVER, m, n, x.k, 1 if relu else 0, _stream(stream)),
+        _check(lib().dfq_linear_mx_variant(variant, *operands, at, ld, code, None, 0, None, 0, MX8, MX_COVER, m, n, x.k, 1 if relu else 0, _stream_here(stream)),
                "dfq_linear_mx_variant")
     return out
 
@@ -494,9 +516,9 @@ def linear_mx_q(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, e
     m, n, operands = _linear_operands(x, w, bias)
     out, q = _new_mx(m, n, elem, x.codes.device, stream) if out is None else _out_mx(out, m, n, elem)
     if variant == LINEAR_AUTO:
-        _check(lib().dfq_linear_mx_q(*operands, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx_q")
+        _check(lib().dfq_linear_mx_q(*operands, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream_here(stream)), "dfq_linear_mx_q")
     else:
-        _check(lib().dfq_linear_mx_variant(variant, *operands, None, 0, 0, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream(stream)), "dfq_linear_mx_variant")
+        _check(lib().dfq_linear_mx_variant(variant, *operands, None, 0, 0, *q, elem, rule, m, n, x.k, 1 if relu else 0, _stream_here(stream)), "dfq_linear_mx_variant")
     return out
 
 
@@ -521,15 +543,15 @@ def rms_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: flo
         out, q = _new_mx(rows, k, elem, x.device, stream) if out is None else _out_mx(out, rows, k, elem)
     elif out is not None:
         raise ValueError("out: nothing is converted with elem=None")
-    y = _new(x.shape, dt, x.device, stream) if want_y else None
+    y = _like(x, stream) if want_y else None
     total, sp, ldsum = sum_out, None, k
     if total is not None:
         sp, ldsum = _out_rows(total, "sum_out", dt, rows, k)
     elif add is not None:
-        total = _new(x.shape, dt, x.device, stream)
+        total = _like(x, stream)
         sp = total.data_ptr()
     _check(lib().dfq_rms_norm_mx(at, ld, a, lda, sp, ldsum, code, wp, wcode, eps, _ptr(y), k, *q, MX8 if elem is None else elem, rule, rows, k,
-                                 _stream(stream)), "dfq_rms_norm_mx")
+                                 _stream_here(stream)), "dfq_rms_norm_mx")
     return out, y, total
 
 
