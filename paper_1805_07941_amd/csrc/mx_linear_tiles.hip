@@ -45,7 +45,7 @@ struct Operand {
 };
 
 // chunks of scales in LDS: chunk s / SPC + 1 is loaded with step s, up to NST steps ahead of the one that is read
-constexpr int scale_chunks(int nst, int spc) { return (nst + spc - 1) / spc + 2; }
+constexpr int scale_chunks(int nst, int spc) { return (nst + spc - 1) / spc + 2 <= 4 ? 4 : 8; }
 
 // where a row's words of a chunk of scales are
 __device__ __forceinline__ int scale_key(int row) { return (row >> 3) & 3; }
@@ -59,7 +59,7 @@ struct Frag32 {
     unsigned scale, scale1;
 };
 
-template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST>
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST, bool WHOLE>
 __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(TileParams prm)
 {
     constexpr int NW = WM * WN;
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     // load j of a chunk
     auto issue_scales = [&](int j, int chunk) __attribute__((always_inline)) {
         const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane(
-            (int)(lds_base + NST * kStage + (unsigned)(chunk % NCH) * kChunk + (unsigned)(wave + NW * j) * 256u));
+            (int)(lds_base + NST * kStage + (unsigned)(chunk & (NCH - 1)) * kChunk + (unsigned)(wave + NW * j) * 256u));
         const bool x = j < BM / (16 * NW);
         const v4i r = {x ? xsr.x : wsr.x, x ? xsr.y : wsr.y, x ? xsr.z : wsr.z, wsr.w};
         const unsigned moved = x ? (unsigned)j * (16 * NW) * ldxs : (unsigned)(j - BM / (16 * NW)) * (16 * NW) * ldws;
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     // A step's loads are issued one or two at a time between matrix instructions - a burst of them fills the memory pipeline's queue and
     // holds up the wavefront - from slot 0 behind the barrier that frees the stage on: over the rest of the step's last part, and with
     // four parts to a step over the first part of the next step too.  (EXACT: registers for one burst only.)
-    constexpr int kLate = EXACT || TM == 1 ? 1 : TM - 1, kSlots = kLate + (KK == 4 && !EXACT ? TM : 0);
+    constexpr int kLate = EXACT || WHOLE || TM == 1 ? 1 : TM - 1, kSlots = kLate + (KK == 4 && !EXACT && !WHOLE ? TM : 0);
     auto issue_slot = [&](int step, int stage, auto slot) __attribute__((always_inline)) {
         constexpr int s = decltype(slot)::value;
         issue(step, stage, std::integral_constant<int, s * LPS / kSlots>{}, std::integral_constant<int, (s + 1) * LPS / kSlots>{});
@@ -160,14 +160,12 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
 
     // ---- consumer
     const int wm0 = wave % WM * (BM / WM), wn0 = wave / WM * (BN / WN);
-    Frag32<EW, EXACT> fw[2][TN];                                       // this part's and the next one's
-    Frag32<EX, EXACT> fx[TM];                                          // each read again as soon as it is multiplied
     // Addresses: a lane's row and the key of its pieces are the same in every group of 32 rows; the groups differ by constants.
     const unsigned xlane = (unsigned)(wm0 + l32) * OX::kRow, wlane = (unsigned)(BM * OX::kRow + (wn0 + l32) * OW::kRow);
     const unsigned xkey = OX::place(l32, 0) * 16, wkey = OW::place(l32, 0) * 16;
     const unsigned skey = scale_key(l32) * 4;
     const unsigned xslane = (unsigned)(NST * kStage + (wm0 + l32) * 16), wslane = (unsigned)(NST * kStage + (BM + wn0 + l32) * 16);
-    auto read_rows = [&](auto &f, auto op, unsigned at, unsigned key, unsigned scale_at, int kk, unsigned b0, unsigned b1) __attribute__((always_inline)) {
+    auto read_rows = [&](auto &f, auto op, unsigned at, unsigned key, unsigned scale_at, int kk) __attribute__((always_inline)) {
         constexpr bool wide = decltype(op)::kRow * 8 / KS == 8;
         if constexpr (wide) {
             f.lo = *(const v4i *)(lds + at + (((4 * kk + h) * 16) ^ key));
@@ -180,33 +178,40 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
             f.lo = *(const v4i *)(lds + at + (((2 * kk + h) * 16) ^ key));
         }
         if constexpr (EXACT) {
-            f.scale = *(const unsigned char *)(lds + scale_at) & b0;
-            f.scale1 = *(const unsigned char *)(lds + scale_at + 1) & b1;
+            f.scale = *(const unsigned char *)(lds + scale_at);
+            f.scale1 = *(const unsigned char *)(lds + scale_at + 1);
         } else {
-            f.scale = *(const unsigned char *)(lds + scale_at + h) & b0;
+            f.scale = *(const unsigned char *)(lds + scale_at + h);
         }
     };
-    struct Part {                                                      // 64 values of the reduction axis
+    // 64 values of the reduction axis: part kk of a step
+    struct Part {
         int kk;
-        unsigned rows, scales, b0, b1;
+        unsigned rows, scales;
     };
     auto part_of = [&](int step, int stage, int kk) __attribute__((always_inline)) {
         const int block = (step * KK + kk) * 2;                        // the first of the two
-        return Part{kk, (unsigned)stage * kStage, (unsigned)(step / SPC % NCH * kChunk) + ((unsigned)(block & 12) ^ skey) + (unsigned)(block & 2),
-                    block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, block + 1 < prm.nb ? 255u : 0u};
+        return Part{kk, (unsigned)stage * kStage, (unsigned)((step / SPC & (NCH - 1)) * kChunk) + ((unsigned)(block & 12) ^ skey) + (unsigned)(block & 2)};
     };
     auto read_w = [&](Frag32<EW, EXACT> &f, int n, const Part &p) __attribute__((always_inline)) {
-        read_rows(f, OW{}, p.rows + wlane + n * 32 * OW::kRow, wkey, p.scales + wslane + n * 512, p.kk, p.b0, p.b1);
+        read_rows(f, OW{}, p.rows + wlane + n * 32 * OW::kRow, wkey, p.scales + wslane + n * 512, p.kk);
     };
-    auto read_x = [&](int m, const Part &p) __attribute__((always_inline)) {
-        read_rows(fx[m], OX{}, p.rows + xlane + m * 32 * OX::kRow, xkey, p.scales + xslane + m * 512, p.kk, p.b0, p.b1);
+    auto read_x = [&](Frag32<EX, EXACT> &f, int m, const Part &p) __attribute__((always_inline)) {
+        read_rows(f, OX{}, p.rows + xlane + m * 32 * OX::kRow, xkey, p.scales + xslane + m * 512, p.kk);
+    };
+    // which bytes of this lane's scales count in a part (taken where they are used, not where they are read: no wait there)
+    struct Counts {
+        unsigned b0, b1;
+    };
+    auto counts_of = [&](int step, int kk) __attribute__((always_inline)) {
+        const int block = (step * KK + kk) * 2;
+        return Counts{block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, block + 1 < prm.nb ? 255u : 0u};
     };
     v16f acc[TN][TM] = {};
-    auto multiply = [&](const Frag32<EW, EXACT> (&w)[TN], int m) __attribute__((always_inline)) {
-        const auto &x = fx[m];
+    auto multiply = [&](const Frag32<EW, EXACT> (&w)[TN], const Frag32<EX, EXACT> &x, int m, const Counts &c) __attribute__((always_inline)) {
         if constexpr (EXACT) {
             auto bf16 = [&](const auto &g, bool wide, int i) __attribute__((always_inline)) {
-                const float s = __uint_as_float((i < 2 ? g.scale : g.scale1) << 23);
+                const float s = __uint_as_float((i < 2 ? g.scale & c.b0 : g.scale1 & c.b1) << 23);
                 const v4i q = wide && i >= 2 ? g.hi : g.lo;
                 return wide ? bf16_of_mx8(q[2 * (i & 1)], q[2 * (i & 1) + 1], s) : bf16_of_mx4(q[i], s);
             };
@@ -224,7 +229,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
 #pragma unroll
             for (int n = 0; n < TN; n++)
                 acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n].lo, w[n].hi, EW == kMx8), codes(x.lo, x.hi, EX == kMx8), acc[n][m], FW, FX, 0,
-                                                                            (int)w[n].scale, 0, (int)x.scale);
+                                                                            (int)(w[n].scale & c.b0), 0, (int)(x.scale & c.b0));
         }
     };
     // completes this wavefront's LDS reads, waits for no vector-memory operation
@@ -238,43 +243,87 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     issue(NST - 1, NST - 1, None{}, std::integral_constant<int, kFirst>{});
     wait_loads<(NST - 2) * LPS + kFirst>();
     ring_barrier();
-    {
-        const Part p = part_of(0, 0, 0);
+    if constexpr (WHOLE) {
+        // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets.
+        struct Set {
+            Frag32<EW, EXACT> w[KK][TN];
+            Frag32<EX, EXACT> x[KK][TM];
+        };
+        Set sets[2];
+        auto read_step = [&](Set &f, int step, int stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < TN; n++) read_w(fw[0][n], n, p);
+            for (int kk = 0; kk < KK; kk++) {
+                const Part p = part_of(step, stage, kk);
 #pragma unroll
-        for (int m = 0; m < TM; m++) read_x(m, p);
-    }
-
-    // A step's KK parts.  A token group's operands are read again for the next part as soon as they are multiplied, the features'
-    // into the other of two sets.  Behind the first products of a step's last part every read of this step has been made: the
-    // wavefronts meet there, the next step having arrived, and the stage is filled again.  Steps past the last are all out of range:
-    // their loads bring zeros, touch no memory, and keep one form of the loop.
-    for (int i = 0, stage = 0; i < steps; i++) {
-        const int next = stage + 1 == NST ? 0 : stage + 1, last = stage == 0 ? NST - 1 : stage - 1;
-        static_for<KK>([&](auto part) __attribute__((always_inline)) {
-            constexpr int kk = decltype(part)::value;
-            const Part p = kk + 1 < KK ? part_of(i, stage, kk + 1) : part_of(i + 1, next, 0);
-            static_for<TM>([&](auto group) __attribute__((always_inline)) {
-                constexpr int m = decltype(group)::value;
-                multiply(fw[kk & 1], m);
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (m == 0) {
-                    if constexpr (kk == KK - 1) {
-                        wait_loads<(NST - 2) * LPS>();
-                        ring_barrier();
+                for (int n = 0; n < TN; n++) read_w(f.w[kk][n], n, p);
+#pragma unroll
+                for (int m = 0; m < TM; m++) read_x(f.x[kk][m], m, p);
+            }
+        };
+        auto do_step = [&](Set &now, Set &then, int i, int stage, int next) __attribute__((always_inline)) {
+            wait_loads<(NST - 2) * LPS>();
+            ring_barrier();                                            // (and every wavefront has read step i)
+            read_step(then, i + 1, next);
+            issue(i + NST, stage, None{}, std::integral_constant<int, LPS>{});
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int kk = 0; kk < KK; kk++) {
+                const Counts c = counts_of(i, kk);
+#pragma unroll
+                for (int m = 0; m < TM; m++) multiply(now.w[kk], now.x[kk][m], m, c);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        read_step(sets[0], 0, 0);
+        int stage = 0;
+        for (int i = 0; i < steps; i += 2) {
+            // (a step past the last multiplies zeros)
+            const int s1 = stage + 1 == NST ? 0 : stage + 1, s2 = s1 + 1 == NST ? 0 : s1 + 1;
+            do_step(sets[0], sets[1], i, stage, s1);
+            do_step(sets[1], sets[0], i + 1, s1, s2);
+            stage = s2;
+        }
+    } else {
+        Frag32<EW, EXACT> fw[2][TN];                                   // this part's and the next one's
+        Frag32<EX, EXACT> fx[TM];                                      // each read again as soon as it is multiplied
+        {
+            const Part p = part_of(0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < TN; n++) read_w(fw[0][n], n, p);
+#pragma unroll
+            for (int m = 0; m < TM; m++) read_x(fx[m], m, p);
+        }
+        // A step's KK parts.  A token group's operands are read again for the next part as soon as they are multiplied, the features'
+        // into the other of two sets.  Behind the first products of a step's last part every read of this step has been made: the
+        // wavefronts meet there, the next step having arrived, and the stage is filled again.  Steps past the last are all out of
+        // range: their loads bring zeros, touch no memory, and keep one form of the loop.
+        for (int i = 0, stage = 0; i < steps; i++) {
+            const int next = stage + 1 == NST ? 0 : stage + 1, last = stage == 0 ? NST - 1 : stage - 1;
+            static_for<KK>([&](auto part) __attribute__((always_inline)) {
+                constexpr int kk = decltype(part)::value;
+                const Part p = kk + 1 < KK ? part_of(i, stage, kk + 1) : part_of(i + 1, next, 0);
+                const Counts c = counts_of(i, kk);
+                static_for<TM>([&](auto group) __attribute__((always_inline)) {
+                    constexpr int m = decltype(group)::value;
+                    multiply(fw[kk & 1], fx[m], m, c);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (m == 0) {
+                        if constexpr (kk == KK - 1) {
+                            wait_loads<(NST - 2) * LPS>();
+                            ring_barrier();
+                        }
+#pragma unroll
+                        for (int n = 0; n < TN; n++) read_w(fw[~kk & 1][n], n, p);
                     }
-#pragma unroll
-                    for (int n = 0; n < TN; n++) read_w(fw[~kk & 1][n], n, p);
-                }
-                read_x(m, p);
-                constexpr int late = TM == 1 ? m : m - 1;
-                if constexpr (kk == KK - 1 && late >= 0 && late < kLate) issue_slot(i + NST, stage, std::integral_constant<int, late < 0 ? 0 : late>{});
-                if constexpr (kk == 0 && kSlots > kLate) issue_slot(i + NST - 1, last, std::integral_constant<int, kLate + m>{});
-                __builtin_amdgcn_sched_barrier(0);
+                    read_x(fx[m], m, p);
+                    constexpr int late = TM == 1 ? m : m - 1;
+                    if constexpr (kk == KK - 1 && late >= 0 && late < kLate) issue_slot(i + NST, stage, std::integral_constant<int, late < 0 ? 0 : late>{});
+                    if constexpr (kk == 0 && kSlots > kLate) issue_slot(i + NST - 1, last, std::integral_constant<int, kLate + m>{});
+                    __builtin_amdgcn_sched_barrier(0);
+                });
             });
-        });
-        stage = next;
+            stage = next;
+        }
     }
     wait_loads<0>();
 
@@ -314,14 +363,14 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     }
 }
 
-template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST>
+template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST, bool WHOLE>
 hipError_t run(const LinearMxArgs &a, hipStream_t st)
 {
     constexpr int KS = EX == kMx4 && EW == kMx4 ? 256 : 128;
     constexpr int kParts = 512 / KS * WM * WN;                         // loads of scales come in multiples of this
     constexpr int kLds = NST * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + scale_chunks(NST, 512 / KS) * (((BM + BN) / 16 + kParts - 1) / kParts * kParts * 256);
     static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
-    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN, OCC, NST>;
+    const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN, OCC, NST, WHOLE>;
     static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (allowed != hipSuccess) return allowed;
     TileParams p{a, (a.K + kMxBlock - 1) / kMxBlock};
@@ -343,9 +392,9 @@ template <int EX, int EW, bool EXACT>
 hipError_t by_shape(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 {
     switch (form) {
-        case LinearMxForm::Tile64x64: return run<EX, EW, EXACT, 64, 64, 2, 2, 3, 3>(a, st);
-        case LinearMxForm::Tile128x128: return run<EX, EW, EXACT, 128, 128, 2, 2, 2, 2>(a, st);
-        case LinearMxForm::Tile256x256: return run<EX, EW, EXACT, 256, 256, 2, 4, 2, 2>(a, st);
+        case LinearMxForm::Tile64x64: return run<EX, EW, EXACT, 64, 64, 2, 2, 3, 3, true>(a, st);
+        case LinearMxForm::Tile128x128: return run<EX, EW, EXACT, 128, 128, 2, 2, 2, 2, true>(a, st);
+        case LinearMxForm::Tile256x256: return run<EX, EW, EXACT, 256, 256, 2, 4, 2, 2, false>(a, st);
         default: return hipErrorInvalidValue;
     }
 }
