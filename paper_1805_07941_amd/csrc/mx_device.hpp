@@ -187,7 +187,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t u)
 }
 
 // Octet o of a row, held by lane o % 4 of a quad with the other octets of its block: converted and stored.  All four lanes of the
-// quad come here (those behind K with zeros).  nb: blocks of the row; the last one's first lane clears the scales' padding too.
+// quad come here (those behind K with zeros).  nb: blocks of the row; the last one's first lane clears the scales' padding too (nb < 0:
+// there is none).
 template <int ELEM>
 __device__ __forceinline__ void mx_store_octet(const float (&v)[8], uint8_t *codes, uint8_t *scales, int o, int nb, bool cover)
 {

@@ -120,6 +120,21 @@ __device__ __forceinline__ v4f multiply16(const Frag16<EW, EXACT> &w, const Frag
     }
 }
 
+// What becomes of results: dfq_dtype's types, or converted.
+constexpr int kToMx4 = 3, kToMx8 = 4;
+
+// f(kind) with the kind of a call's results as a type
+template <class F>
+__device__ __forceinline__ void with_kind(const LinearMxArgs &a, F &&f)
+{
+    const int kind = a.q.codes ? (a.q.elem == kMx8 ? kToMx8 : kToMx4) : a.dtype;
+    if (kind == kBF16) f(std::integral_constant<int, kBF16>{});
+    else if (kind == kF16) f(std::integral_constant<int, kF16>{});
+    else if (kind == kF32) f(std::integral_constant<int, kF32>{});
+    else if (kind == kToMx8) f(std::integral_constant<int, kToMx8>{});
+    else f(std::integral_constant<int, kToMx4>{});
+}
+
 // The end of results, an octet (features 8o .. 8o + 7) of one token at a time: bias, ReLU, rounding and the store.  A lane keeps its
 // octet from token to token.  Converted results: the four lanes of a quad hold a block and come here together.
 struct OctetEnd {
@@ -133,6 +148,8 @@ struct OctetEnd {
 #pragma unroll
         for (int j = 0; j < 8; j++) bias[j] = a.bias && o * 8 + j < a.N ? a.bias[o * 8 + j] : 0.0f;
     }
+    // WHOLE: the octet and its block are within N, the rows on multiples of 16, and no scales' padding is to be cleared here
+    template <int KIND, bool WHOLE>
     __device__ __forceinline__ void put(float (&v)[8], const LinearMxArgs &a, size_t m) const
     {
         if (a.bias) {
@@ -143,19 +160,17 @@ struct OctetEnd {
 #pragma unroll
             for (int j = 0; j < 8; j++) v[j] = relu_f32(v[j]);
         }
-        if (a.q.codes) {
-            if (o >= blocks * 4) return;                          // (whole quads)
-            if (o * 8 + 8 > a.N) {
+        if constexpr (KIND == kToMx4 || KIND == kToMx8) {
+            if (!WHOLE) {
+                if (o >= blocks * 4) return;                      // (whole quads)
 #pragma unroll
                 for (int j = 0; j < 8; j++) v[j] = o * 8 + j < a.N ? v[j] : 0.0f;
             }
-            uint8_t *codes = a.q.codes + m * a.q.ldc, *scales = a.q.scales + m * a.q.lds;
-            if (a.q.elem == kMx8) mx_store_octet<kMx8>(v, codes, scales, o, blocks, a.cover);
-            else mx_store_octet<kMx4>(v, codes, scales, o, blocks, a.cover);
+            mx_store_octet<KIND == kToMx8 ? kMx8 : kMx4>(v, a.q.codes + m * a.q.ldc, a.q.scales + m * a.q.lds, o, WHOLE ? -1 : blocks, a.cover);
+        } else if constexpr (WHOLE) {
+            store_octet<KIND>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, o * 8 + 8, true);
         } else if (o * 8 < a.N) {
-            if (a.dtype == kF32) store_octet<kF32>(v, (char *)a.y + m * a.ldy * 4, o, a.N, vec);
-            else if (a.dtype == kBF16) store_octet<kBF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, vec);
-            else store_octet<kF16>(v, (char *)a.y + m * a.ldy * 2, o, a.N, vec);
+            store_octet<KIND>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, a.N, vec);
         }
     }
 };

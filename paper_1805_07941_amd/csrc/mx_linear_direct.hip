@@ -84,21 +84,23 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_direct_kernel(LinearMxArgs 
     __syncthreads();
 
     constexpr int kOctets = F / 8;
-    for (int i = threadIdx.x; i < T * kOctets; i += NW * 64) {
-        const int t = i / kOctets, o = i % kOctets;
-        const size_t m = m0 + t;
-        float v[8] = {};
-#pragma unroll 2
-        for (int w = 0; w < NW; w++) {
-            const v4f *p = (const v4f *)&part[w][t][o * 8];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                v[j] += p[0][j];
-                v[4 + j] += p[1][j];
+    with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+        for (int i = threadIdx.x; i < T * kOctets; i += NW * 64) {
+            const int t = i / kOctets, o = i % kOctets;
+            const size_t m = m0 + t;
+            float v[8] = {};
+    #pragma unroll 2
+            for (int w = 0; w < NW; w++) {
+                const v4f *p = (const v4f *)&part[w][t][o * 8];
+    #pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    v[j] += p[0][j];
+                    v[4 + j] += p[1][j];
+                }
             }
+            if (m < a.M) OctetEnd(a, n0 / 8 + o).put<decltype(kind)::value, false>(v, a, m);
         }
-        if (m < a.M) OctetEnd(a, n0 / 8 + o).put(v, a, m);
-    }
+    });
 }
 
 template <int EX, int EW, bool EXACT, int FT, int TT, int NW, int U>

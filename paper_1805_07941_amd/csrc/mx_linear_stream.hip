@@ -122,20 +122,22 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_stream_kernel(LinearMxArgs 
         for (int t = 0; t < TT; t++) *(v4f *)&part[(t * 16 + l16) * kPad + f * 16 + g * 4] = acc[f][t];
     __syncthreads();
     constexpr int kOctets = F / 8;
-    for (int i = threadIdx.x; i < T * kOctets; i += NW * 64) {
-        const int t = i / kOctets, o = i % kOctets;
-        float v[8] = {};
-#pragma unroll 2
-        for (int w = 0; w < NW; w++) {
-            const v4f *p = (const v4f *)(lds + w * NST * kStage + (t * kPad + o * 8) * 4);
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                v[j] += p[0][j];
-                v[4 + j] += p[1][j];
+    with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+        for (int i = threadIdx.x; i < T * kOctets; i += NW * 64) {
+            const int t = i / kOctets, o = i % kOctets;
+            float v[8] = {};
+    #pragma unroll 2
+            for (int w = 0; w < NW; w++) {
+                const v4f *p = (const v4f *)(lds + w * NST * kStage + (t * kPad + o * 8) * 4);
+    #pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    v[j] += p[0][j];
+                    v[4 + j] += p[1][j];
+                }
             }
+            if (m0 + t < a.M) OctetEnd(a, n0 / 8 + o).put<decltype(kind)::value, false>(v, a, m0 + t);
         }
-        if (m0 + t < a.M) OctetEnd(a, n0 / 8 + o).put(v, a, m0 + t);
-    }
+    });
 }
 
 template <int EX, int EW, bool EXACT, int FT, int TT, int NW, int NST>

@@ -335,32 +335,42 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     float *mine = (float *)lds + wave * 32 * kPad;
     constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
     const OctetEnd end(a, (n0 + wn0) / 8 + lane % kOctets);
-#pragma unroll 1
-    for (int m = 0; m < TM; m++) {
-#pragma unroll
-        for (int mm = 0; mm < TM; mm++) {
-            if (mm != m) continue;
+    const bool inside = mrows == BM && n0 + BN <= a.N && (a.q.codes ? n0 + BN < a.N || a.N % 128 == 0 : end.vec);
+    with_kind(a, [&](auto kind) __attribute__((always_inline)) {
+        static_for<TM>([&](auto group) __attribute__((always_inline)) {
+            constexpr int m = decltype(group)::value;
 #pragma unroll
             for (int n = 0; n < TN; n++)
 #pragma unroll
                 for (int q = 0; q < 4; q++)
-                    *(v4f *)&mine[l32 * kPad + n * 32 + 16 * h + 4 * q] = v4f{acc[n][mm][4 * q], acc[n][mm][4 * q + 1], acc[n][mm][4 * q + 2], acc[n][mm][4 * q + 3]};
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int it = 0; it < 32; it += kTokens) {
-            const int token = it + lane / kOctets;
-            const v4f *p = (const v4f *)&mine[token * kPad + lane % kOctets * 8];
-            float v[8];
+                    *(v4f *)&mine[l32 * kPad + n * 32 + 16 * h + 4 * q] = v4f{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+            __builtin_amdgcn_wave_barrier();
+            auto octet = [&](float (&v)[8], int token) __attribute__((always_inline)) {
+                const v4f *p = (const v4f *)&mine[token * kPad + lane % kOctets * 8];
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                v[j] = p[0][j];
-                v[4 + j] = p[1][j];
+                for (int j = 0; j < 4; j++) {
+                    v[j] = p[0][j];
+                    v[4 + j] = p[1][j];
+                }
+            };
+            const int first = wm0 + m * 32 + lane / kOctets;
+            if (inside) {
+                float v[32 / kTokens][8];
+#pragma unroll
+                for (int it = 0; it < 32 / kTokens; it++) octet(v[it], it * kTokens + lane / kOctets);
+#pragma unroll
+                for (int it = 0; it < 32 / kTokens; it++) end.put<decltype(kind)::value, true>(v[it], a, m0 + first + it * kTokens);
+            } else {
+#pragma unroll 1
+                for (int it = 0; it < 32; it += kTokens) {
+                    float v[8];
+                    octet(v, it + lane / kOctets);
+                    if (first + it < mrows) end.put<decltype(kind)::value, false>(v, a, m0 + first + it);
+                }
             }
-            if (wm0 + m * 32 + token < mrows) end.put(v, a, m0 + wm0 + m * 32 + token);
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
+            __builtin_amdgcn_wave_barrier();
+        });
+    });
 }
 
 template <int EX, int EW, bool EXACT, int BM, int BN, int WM, int WN, int OCC, int NST, bool WHOLE>
