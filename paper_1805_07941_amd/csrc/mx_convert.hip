@@ -30,20 +30,36 @@ __global__ void __launch_bounds__(kBlock) quantize_mx_kernel(const char *__restr
     mx_store_octet<ELEM>(v, codes + (size_t)row * ldc, scales + (size_t)row * lds, o, nb, cover);
 }
 
+// A lane stores 16 bytes: eight values of a 16-bit type or four floats (`units` of them in a row)
 template <int DT, int ELEM>
 __global__ void __launch_bounds__(kBlock) dequantize_mx_kernel(const uint8_t *__restrict__ codes, size_t ldc, const uint8_t *__restrict__ scales, size_t lds,
-                                                               char *__restrict__ x, size_t ldx, int K, int no, unsigned total, FastDiv div, int vec)
+                                                               char *__restrict__ x, size_t ldx, int K, int units, unsigned total, FastDiv div, int vec)
 {
+    constexpr int N = DT == kF32 ? 4 : 8;
     const unsigned t = blockIdx.x * kBlock + threadIdx.x;
     if (t >= total) return;
-    const int row = fastdiv((int)t, div), o = (int)t - row * no;
-    const uint8_t *c = codes + (size_t)row * ldc;
+    const int row = fastdiv((int)t, div), o = (int)t - row * units;
+    const uint8_t *c = codes + (size_t)row * ldc + (size_t)o * (N * (ELEM == kMx8 ? 8 : 4) / 8);
     uint2 w = make_uint2(0u, 0u);
-    if constexpr (ELEM == kMx4) w.x = ((const uint32_t *)c)[o];
-    else w = ((const uint2 *)c)[o];
-    float v[8];
-    mx_values<ELEM>(v, w, scales[(size_t)row * lds + (o >> 2)]);
-    store_octet<DT>(v, x + (size_t)row * ldx, o, K, vec);
+    if constexpr (ELEM == kMx8 && N == 8) w = *(const uint2 *)c;
+    else if constexpr (ELEM == kMx4 && N == 4) w.x = *(const uint16_t *)c;
+    else w.x = *(const uint32_t *)c;
+    float v[N];
+    mx_values<ELEM>(v, w, scales[(size_t)row * lds + o * N / kMxBlock]);
+    char *to = x + (size_t)row * ldx;
+    if constexpr (DT == kF32) {
+        float *p = (float *)to + o * 4;
+        const int left = K - o * 4;
+        if (vec && left >= 4) {
+            store_as<true>((f32x4 *)p, f32x4{v[0], v[1], v[2], v[3]});
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (i < left) p[i] = v[i];
+        }
+    } else {
+        store_octet<DT, true>(v, to, o, K, vec);
+    }
 }
 
 template <int DT>
@@ -66,16 +82,17 @@ hipError_t run_quantize(const MxRows &x, const MxTensor &q, bool cover, hipStrea
 template <int DT>
 hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 {
-    const int no = (x.K + 7) / 8;
-    const size_t most = (size_t)(kMostOctets / no);
+    constexpr int N = DT == kF32 ? 4 : 8;
+    const int units = (x.K + N - 1) / N;
+    const size_t most = (size_t)(kMostOctets / units);
     const int vec = vec16(x.p, x.ld * dtype_bytes<DT>());
     for (size_t r = 0; r < x.rows; r += most) {
         const size_t rows = x.rows - r < most ? x.rows - r : most;
-        const unsigned total = (unsigned)(rows * no);
+        const unsigned total = (unsigned)(rows * units);
         char *xp = (char *)x.p + r * x.ld * dtype_bytes<DT>();
         const auto kernel = q.elem == kMx8 ? dequantize_mx_kernel<DT, kMx8> : dequantize_mx_kernel<DT, kMx4>;
-        kernel<<<(total + kBlock - 1) / kBlock, kBlock, 0, st>>>(q.codes + r * q.ldc, q.ldc, q.scales + r * q.lds, q.lds, xp, x.ld * dtype_bytes<DT>(), x.K, no,
-                                                                 total, make_fastdiv(no), vec);
+        kernel<<<(total + kBlock - 1) / kBlock, kBlock, 0, st>>>(q.codes + r * q.ldc, q.ldc, q.scales + r * q.lds, q.lds, xp, x.ld * dtype_bytes<DT>(), x.K, units,
+                                                                 total, make_fastdiv(units), vec);
     }
     return hipGetLastError();
 }
@@ -136,7 +153,7 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
     const float r = 1.0f / sqrtf(sq / (float)K + p.a.eps);
 
     auto finish = [&](float (&v)[8], int o) __attribute__((always_inline)) {
-        if (p.a.sum) store_octet<DT>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K, p.vec_sum);
+        if (p.a.sum) store_octet<DT, true>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K, p.vec_sum);
         float w[8];
         if (!p.a.weight) {
 #pragma unroll
@@ -148,7 +165,7 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
         }
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * r * w[i] : 0.0f;      // (zeros behind K whatever r is)
-        if (p.a.y) store_octet<DT>(v, (char *)p.a.y + row * p.a.ldy * B, o, K, p.vec_y);
+        if (p.a.y) store_octet<DT, true>(v, (char *)p.a.y + row * p.a.ldy * B, o, K, p.vec_y);
         if (p.a.q.codes) mx_store_octet<ELEM>(v, p.a.q.codes + row * p.a.q.ldc, p.a.q.scales + row * p.a.q.lds, o, p.nb, p.a.cover);
     };
     if constexpr (V > 0) {

@@ -81,18 +81,30 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b)
     }
 }
 
-// the values of an octet rounded to the row's type and stored; nothing past K
-template <int DT>
+// NT: results that are written once and too many for a cache to hold go past it
+template <bool NT, class T>
+__device__ __forceinline__ void store_as(T *p, const T &v)
+{
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// the values of an octet rounded to the row's type and stored; nothing past K.  (float32: two stores that take turns in a cache line,
+// which do not go past the cache: 8192 x 8192 converted back 64 us, past it 104.)
+template <int DT, bool NT = false>
 __device__ __forceinline__ void store_octet(const float (&v)[8], void *row, int o, int K, bool vec)
 {
     char *p = (char *)row + (size_t)o * 8 * dtype_bytes<DT>();
     const int left = K - o * 8;
     if (vec && left >= 8) {
         if constexpr (DT == kF32) {
-            ((float4 *)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            ((float4 *)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            ((f32x4 *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+            ((f32x4 *)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
         } else {
-            *(uint4 *)p = make_uint4(pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7]));
+            store_as<NT>((u32x4 *)p, u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])});
         }
         return;
     }
@@ -152,25 +164,29 @@ __device__ __forceinline__ uint2 mx_codes(const float (&v)[8], int s, bool cover
     }
 }
 
-// ---- an octet of codes at scale byte s as floats (exact; products below 2^-149 do not occur)
-template <int ELEM>
-__device__ __forceinline__ void mx_values(float (&v)[8], uint2 w, int s)
+// ---- N codes (8 or 4; the words that hold them) at scale byte s as floats (exact; products below 2^-149 do not occur)
+template <int ELEM, int N>
+__device__ __forceinline__ void mx_values(float (&v)[N], uint2 w, int s)
 {
     const float scale = __uint_as_float((uint32_t)s << 23);
-    v2f f[4];
+    v2f f[N / 2];
     if constexpr (ELEM == kMx4) {
         f[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 0);
         f[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 1);
-        f[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 2);
-        f[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 3);
+        if constexpr (N == 8) {
+            f[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 2);
+            f[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, scale, 3);
+        }
     } else {
         f[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, scale, false);
         f[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, scale, true);
-        f[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, scale, false);
-        f[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, scale, true);
+        if constexpr (N == 8) {
+            f[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, scale, false);
+            f[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, scale, true);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < N / 2; i++) {
         v[2 * i] = s == 255 ? __uint_as_float(0x7fc00000u) : f[i][0];
         v[2 * i + 1] = s == 255 ? __uint_as_float(0x7fc00000u) : f[i][1];
     }
@@ -189,7 +205,7 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t u)
 // Octet o of a row, held by lane o % 4 of a quad with the other octets of its block: converted and stored.  All four lanes of the
 // quad come here (those behind K with zeros).  nb: blocks of the row; the last one's first lane clears the scales' padding too (nb < 0:
 // there is none).
-template <int ELEM>
+template <int ELEM, bool NT = false>
 __device__ __forceinline__ void mx_store_octet(const float (&v)[8], uint8_t *codes, uint8_t *scales, int o, int nb, bool cover)
 {
     uint32_t u = 0;
@@ -197,8 +213,8 @@ __device__ __forceinline__ void mx_store_octet(const float (&v)[8], uint8_t *cod
     for (int i = 0; i < 8; i++) u = max(u, magnitude_bits(v[i]));
     const int s = mx_scale_byte<ELEM>(quad_max(u), cover);
     const uint2 w = mx_codes<ELEM>(v, s, cover);
-    if constexpr (ELEM == kMx4) ((uint32_t *)codes)[o] = w.x;
-    else ((uint2 *)codes)[o] = w;
+    if constexpr (ELEM == kMx4) store_as<NT>((uint32_t *)codes + o, w.x);
+    else store_as<NT>((u32x2 *)codes + o, u32x2{w.x, w.y});
     if ((o & 3) == 0) {
         const int b = o >> 2;
         scales[b] = (uint8_t)s;

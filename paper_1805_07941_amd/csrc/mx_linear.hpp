@@ -149,7 +149,7 @@ struct OctetEnd {
         for (int j = 0; j < 8; j++) bias[j] = a.bias && o * 8 + j < a.N ? a.bias[o * 8 + j] : 0.0f;
     }
     // WHOLE: the octet and its block are within N, the rows on multiples of 16, and no scales' padding is to be cleared here
-    template <int KIND, bool WHOLE>
+    template <int KIND, bool WHOLE, bool NT = false>
     __device__ __forceinline__ void put(float (&v)[8], const LinearMxArgs &a, size_t m) const
     {
         if (a.bias) {
@@ -166,9 +166,9 @@ struct OctetEnd {
 #pragma unroll
                 for (int j = 0; j < 8; j++) v[j] = o * 8 + j < a.N ? v[j] : 0.0f;
             }
-            mx_store_octet<KIND == kToMx8 ? kMx8 : kMx4>(v, a.q.codes + m * a.q.ldc, a.q.scales + m * a.q.lds, o, WHOLE ? -1 : blocks, a.cover);
+            mx_store_octet<KIND == kToMx8 ? kMx8 : kMx4, NT>(v, a.q.codes + m * a.q.ldc, a.q.scales + m * a.q.lds, o, WHOLE ? -1 : blocks, a.cover);
         } else if constexpr (WHOLE) {
-            store_octet<KIND>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, o * 8 + 8, true);
+            store_octet<KIND, NT>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, o * 8 + 8, true);
         } else if (o * 8 < a.N) {
             store_octet<KIND>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, a.N, vec);
         }

@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
 #pragma unroll
                 for (int it = 0; it < 32 / kTokens; it++) octet(v[it], it * kTokens + lane / kOctets);
 #pragma unroll
-                for (int it = 0; it < 32 / kTokens; it++) end.put<decltype(kind)::value, true>(v[it], a, m0 + first + it * kTokens);
+                for (int it = 0; it < 32 / kTokens; it++) end.put<decltype(kind)::value, true, BM == 256>(v[it], a, m0 + first + it * kTokens);
             } else {
 #pragma unroll 1
                 for (int it = 0; it < 32; it += kTokens) {
