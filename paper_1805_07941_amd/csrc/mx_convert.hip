@@ -11,29 +11,25 @@ namespace {
 
 constexpr int kBlock = 256;
 
-// every row starts on a multiple of 16 bytes
-inline int vec16(const void *p, size_t ld_bytes) { return ((uintptr_t)p | ld_bytes) % 16 == 0; }
-
 // rows * octets of one launch: 32-bit thread numbers and grids
 constexpr long long kMostOctets = 1LL << 30;
 
 template <int DT, int ELEM>
 __global__ void __launch_bounds__(kBlock) quantize_mx_kernel(const char *__restrict__ x, size_t ldx, uint8_t *__restrict__ codes, size_t ldc,
-                                                             uint8_t *__restrict__ scales, size_t lds, int K, int nb, unsigned total, FastDiv div, int vec,
-                                                             int cover)
+                                                             uint8_t *__restrict__ scales, size_t lds, int K, int nb, unsigned total, FastDiv div, int cover)
 {
     const unsigned t = blockIdx.x * kBlock + threadIdx.x;
     if (t >= total) return;                          // (total is a multiple of 4: whole quads)
     const int row = fastdiv((int)t, div), o = (int)t - row * nb * 4;
     float v[8];
-    load_octet<DT>(v, x + (size_t)row * ldx, o, K, vec);
+    load_octet<DT>(v, x + (size_t)row * ldx, o, K);
     mx_store_octet<ELEM>(v, codes + (size_t)row * ldc, scales + (size_t)row * lds, o, nb, cover);
 }
 
 // A lane stores 16 bytes: eight values of a 16-bit type or four floats (`units` of them in a row)
 template <int DT, int ELEM>
 __global__ void __launch_bounds__(kBlock) dequantize_mx_kernel(const uint8_t *__restrict__ codes, size_t ldc, const uint8_t *__restrict__ scales, size_t lds,
-                                                               char *__restrict__ x, size_t ldx, int K, int units, unsigned total, FastDiv div, int vec)
+                                                               char *__restrict__ x, size_t ldx, int K, int units, unsigned total, FastDiv div)
 {
     constexpr int N = DT == kF32 ? 4 : 8;
     const unsigned t = blockIdx.x * kBlock + threadIdx.x;
@@ -50,15 +46,15 @@ __global__ void __launch_bounds__(kBlock) dequantize_mx_kernel(const uint8_t *__
     if constexpr (DT == kF32) {
         float *p = (float *)to + o * 4;
         const int left = K - o * 4;
-        if (vec && left >= 4) {
-            store_as<true>((f32x4 *)p, f32x4{v[0], v[1], v[2], v[3]});
+        if (left >= 4) {
+            store_as<true>((f32x4_any *)p, f32x4{v[0], v[1], v[2], v[3]});
         } else {
 #pragma unroll
             for (int i = 0; i < 4; i++)
                 if (i < left) p[i] = v[i];
         }
     } else {
-        store_octet<DT, true>(v, to, o, K, vec);
+        store_octet<DT, true>(v, to, o, K);
     }
 }
 
@@ -67,14 +63,13 @@ hipError_t run_quantize(const MxRows &x, const MxTensor &q, bool cover, hipStrea
 {
     const int nb = (x.K + kMxBlock - 1) / kMxBlock;
     const size_t most = (size_t)(kMostOctets / (nb * 4LL));
-    const int vec = vec16(x.p, x.ld * dtype_bytes<DT>());
     for (size_t r = 0; r < x.rows; r += most) {
         const size_t rows = x.rows - r < most ? x.rows - r : most;
         const unsigned total = (unsigned)(rows * nb * 4);
         const char *xp = (const char *)x.p + r * x.ld * dtype_bytes<DT>();
         const auto kernel = q.elem == kMx8 ? quantize_mx_kernel<DT, kMx8> : quantize_mx_kernel<DT, kMx4>;
         kernel<<<(total + kBlock - 1) / kBlock, kBlock, 0, st>>>(xp, x.ld * dtype_bytes<DT>(), q.codes + r * q.ldc, q.ldc, q.scales + r * q.lds, q.lds, x.K,
-                                                                 nb, total, make_fastdiv(nb * 4), vec, cover);
+                                                                 nb, total, make_fastdiv(nb * 4), cover);
     }
     return hipGetLastError();
 }
@@ -85,14 +80,13 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
     constexpr int N = DT == kF32 ? 4 : 8;
     const int units = (x.K + N - 1) / N;
     const size_t most = (size_t)(kMostOctets / units);
-    const int vec = vec16(x.p, x.ld * dtype_bytes<DT>());
     for (size_t r = 0; r < x.rows; r += most) {
         const size_t rows = x.rows - r < most ? x.rows - r : most;
         const unsigned total = (unsigned)(rows * units);
         char *xp = (char *)x.p + r * x.ld * dtype_bytes<DT>();
         const auto kernel = q.elem == kMx8 ? dequantize_mx_kernel<DT, kMx8> : dequantize_mx_kernel<DT, kMx4>;
         kernel<<<(total + kBlock - 1) / kBlock, kBlock, 0, st>>>(q.codes + r * q.ldc, q.ldc, q.scales + r * q.lds, q.lds, xp, x.ld * dtype_bytes<DT>(), x.K, units,
-                                                                 total, make_fastdiv(units), vec);
+                                                                 total, make_fastdiv(units));
     }
     return hipGetLastError();
 }
@@ -102,17 +96,17 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 // for that, the second pass reads x and add again).
 struct NormParams {
     RmsNormArgs a;
-    int nb, vec_x, vec_add, vec_sum, vec_y, vec_w;
+    int nb;
 };
 
 template <int DT>
 __device__ __forceinline__ void load_sum(float (&s)[8], const NormParams &p, size_t row, int o)
 {
     constexpr int B = dtype_bytes<DT>();
-    load_octet<DT>(s, (const char *)p.a.x.p + row * p.a.x.ld * B, o, p.a.x.K, p.vec_x);
+    load_octet<DT>(s, (const char *)p.a.x.p + row * p.a.x.ld * B, o, p.a.x.K);
     if (p.a.add) {
         float t[8];
-        load_octet<DT>(t, (const char *)p.a.add + row * p.a.ldadd * B, o, p.a.x.K, p.vec_add);
+        load_octet<DT>(t, (const char *)p.a.add + row * p.a.ldadd * B, o, p.a.x.K);
 #pragma unroll
         for (int i = 0; i < 8; i++) s[i] += t[i];
     }
@@ -153,19 +147,19 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
     const float r = 1.0f / sqrtf(sq / (float)K + p.a.eps);
 
     auto finish = [&](float (&v)[8], int o) __attribute__((always_inline)) {
-        if (p.a.sum) store_octet<DT, true>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K, p.vec_sum);
+        if (p.a.sum) store_octet<DT, true>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K);
         float w[8];
         if (!p.a.weight) {
 #pragma unroll
             for (int i = 0; i < 8; i++) w[i] = 1.0f;
         } else if (p.a.weight_f32) {
-            load_octet<kF32>(w, p.a.weight, o, K, p.vec_w);
+            load_octet<kF32>(w, p.a.weight, o, K);
         } else {
-            load_octet<DT>(w, p.a.weight, o, K, p.vec_w);
+            load_octet<DT>(w, p.a.weight, o, K);
         }
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * r * w[i] : 0.0f;      // (zeros behind K whatever r is)
-        if (p.a.y) store_octet<DT, true>(v, (char *)p.a.y + row * p.a.ldy * B, o, K, p.vec_y);
+        if (p.a.y) store_octet<DT, true>(v, (char *)p.a.y + row * p.a.ldy * B, o, K);
         if (p.a.q.codes) mx_store_octet<ELEM>(v, p.a.q.codes + row * p.a.q.ldc, p.a.q.scales + row * p.a.q.lds, o, p.nb, p.a.cover);
     };
     if constexpr (V > 0) {
@@ -209,13 +203,7 @@ hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t 
 
 hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st)
 {
-    const int B = a.x.dtype == kF32 ? 4 : 2;
-    NormParams p{a, (a.x.K + kMxBlock - 1) / kMxBlock};
-    p.vec_x = vec16(a.x.p, a.x.ld * B);
-    p.vec_add = vec16(a.add, a.ldadd * B);
-    p.vec_sum = vec16(a.sum, a.ldsum * B);
-    p.vec_y = vec16(a.y, a.ldy * B);
-    p.vec_w = vec16(a.weight, 0);
+    const NormParams p{a, (a.x.K + kMxBlock - 1) / kMxBlock};
     const bool mx8 = a.q.elem == kMx8;
     if (a.x.dtype == kF32) return mx8 ? run_norm<kF32, kMx8>(p, st) : run_norm<kF32, kMx4>(p, st);
     if (a.x.dtype == kBF16) return mx8 ? run_norm<kBF16, kMx8>(p, st) : run_norm<kBF16, kMx4>(p, st);

@@ -27,27 +27,37 @@ constexpr int dtype_bytes() { return DT == kF32 ? 4 : 2; }
 // bytes of a block's codes
 __host__ __device__ constexpr int mx_block_bytes(int elem) { return elem == kMx8 ? 32 : 16; }
 
-// ---- eight consecutive values of a row as floats.  vec: the row's address is a multiple of 16; past K: zeros
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+// the same at any address of their element type: global memory takes 16-byte accesses at any
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+// ---- eight consecutive values of a row as floats; past K: zeros
 template <int DT>
-__device__ __forceinline__ void load_octet(float (&v)[8], const void *row, int o, int K, bool vec)
+__device__ __forceinline__ void load_octet(float (&v)[8], const void *row, int o, int K)
 {
     const char *p = (const char *)row + (size_t)o * 8 * dtype_bytes<DT>();
     const int left = K - o * 8;
-    if (vec && left >= 8) {
+    if (left >= 8) {
         if constexpr (DT == kF32) {
-            const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            const f32x4 a = ((const f32x4_any *)p)[0], b = ((const f32x4_any *)p)[1];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                v[i] = a[i];
+                v[4 + i] = b[i];
+            }
         } else {
-            const uint4 w = *(const uint4 *)p;
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            const u32x4 u = *(const u32x4_any *)p;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 if constexpr (DT == kBF16) {
                     v[2 * i] = __uint_as_float(u[i] << 16);
                     v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
                 } else {
-                    const v2h h = __builtin_bit_cast(v2h, u[i]);
+                    const uint32_t w = u[i];
+                    const v2h h = __builtin_bit_cast(v2h, w);
                     v[2 * i] = (float)h[0];
                     v[2 * i + 1] = (float)h[1];
                 }
@@ -82,29 +92,26 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b)
 }
 
 // NT: results that are written once and too many for a cache to hold go past it
-template <bool NT, class T>
-__device__ __forceinline__ void store_as(T *p, const T &v)
+template <bool NT, class P, class T>
+__device__ __forceinline__ void store_as(P *p, const T &v)
 {
     if constexpr (NT) __builtin_nontemporal_store(v, p);
     else *p = v;
 }
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // the values of an octet rounded to the row's type and stored; nothing past K.  (float32: two stores that take turns in a cache line,
 // which do not go past the cache: 8192 x 8192 converted back 64 us, past it 104.)
 template <int DT, bool NT = false>
-__device__ __forceinline__ void store_octet(const float (&v)[8], void *row, int o, int K, bool vec)
+__device__ __forceinline__ void store_octet(const float (&v)[8], void *row, int o, int K)
 {
     char *p = (char *)row + (size_t)o * 8 * dtype_bytes<DT>();
     const int left = K - o * 8;
-    if (vec && left >= 8) {
+    if (left >= 8) {
         if constexpr (DT == kF32) {
-            ((f32x4 *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-            ((f32x4 *)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+            ((f32x4_any *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+            ((f32x4_any *)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
         } else {
-            store_as<NT>((u32x4 *)p, u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])});
+            store_as<NT>((u32x4_any *)p, u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])});
         }
         return;
     }

@@ -140,15 +140,13 @@ __device__ __forceinline__ void with_kind(const LinearMxArgs &a, F &&f)
 struct OctetEnd {
     float bias[8];
     int o, blocks;
-    bool vec;
 
     __device__ __forceinline__ OctetEnd(const LinearMxArgs &a, int octet) : o(octet), blocks((a.N + kMxBlock - 1) / kMxBlock)
     {
-        vec = ((uintptr_t)a.y | a.ldy * (a.dtype == kF32 ? 4 : 2)) % 16 == 0;
 #pragma unroll
         for (int j = 0; j < 8; j++) bias[j] = a.bias && o * 8 + j < a.N ? a.bias[o * 8 + j] : 0.0f;
     }
-    // WHOLE: the octet and its block are within N, the rows on multiples of 16, and no scales' padding is to be cleared here
+    // WHOLE: the octet and its block are within N, and no scales' padding is to be cleared here
     template <int KIND, bool WHOLE, bool NT = false>
     __device__ __forceinline__ void put(float (&v)[8], const LinearMxArgs &a, size_t m) const
     {
@@ -168,9 +166,9 @@ struct OctetEnd {
             }
             mx_store_octet<KIND == kToMx8 ? kMx8 : kMx4, NT>(v, a.q.codes + m * a.q.ldc, a.q.scales + m * a.q.lds, o, WHOLE ? -1 : blocks, a.cover);
         } else if constexpr (WHOLE) {
-            store_octet<KIND, NT>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, o * 8 + 8, true);
+            store_octet<KIND, NT>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, o * 8 + 8);
         } else if (o * 8 < a.N) {
-            store_octet<KIND>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, a.N, vec);
+            store_octet<KIND>(v, (char *)a.y + m * a.ldy * dtype_bytes<KIND>(), o, a.N);
         }
     }
 };

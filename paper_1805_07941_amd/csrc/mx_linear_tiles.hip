@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     float *mine = (float *)lds + wave * 32 * kPad;
     constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
     const OctetEnd end(a, (n0 + wn0) / 8 + lane % kOctets);
-    const bool inside = mrows == BM && n0 + BN <= a.N && (a.q.codes ? n0 + BN < a.N || a.N % 128 == 0 : end.vec);
+    const bool inside = mrows == BM && n0 + BN <= a.N && (!a.q.codes || n0 + BN < a.N || a.N % 128 == 0);
     with_kind(a, [&](auto kind) __attribute__((always_inline)) {
         static_for<TM>([&](auto group) __attribute__((always_inline)) {
             constexpr int m = decltype(group)::value;
