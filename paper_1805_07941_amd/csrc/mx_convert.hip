@@ -92,8 +92,10 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 }
 
 // ---- root-mean-square norm: s = x + add, y = s / sqrt(mean(s^2) + eps) * weight.
-// One workgroup to a row; a thread holds V octets of the sum in registers between the two passes over it (V == 0: rows too long
-// for that, the second pass reads x and add again).
+// R threads to a row (a wavefront's part, a wavefront or a workgroup), V octets of the sum held in registers between the two passes over it; V == 0: rows too long for that, the second pass reads x and add again.  Bound by the bytes: x and add
+// read, the sum and the codes written (8192 x 8192 bfloat16 to 8 bits, 473 MB: 95 us, 5.0 TB/s; a copy of that size 5.1 to 5.3).
+// The sum goes past the cache; the codes stay, the product behind the norm reads them: 8192 x 8192 codes past it 78 us, but norm and
+// product 518 for 509, 16384 x 4096 with its product 314 for 295.
 struct NormParams {
     RmsNormArgs a;
     int nb;
@@ -112,14 +114,31 @@ __device__ __forceinline__ void load_sum(float (&s)[8], const NormParams &p, siz
     }
 }
 
-template <int DT, int ELEM, int T, int V>
+template <int DT>
+__device__ __forceinline__ void load_weight(float (&w)[8], const NormParams &p, int o)
+{
+    if (!p.a.weight) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = 1.0f;
+    } else if (p.a.weight_f32) {
+        load_octet<kF32>(w, p.a.weight, o, p.a.x.K);
+    } else {
+        load_octet<DT>(w, p.a.weight, o, p.a.x.K);
+    }
+}
+
+// T threads to a workgroup
+template <int DT, int ELEM, int T, int R, int V>
 __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
 {
     constexpr int B = dtype_bytes<DT>();
+    static_assert(R <= T && (R <= 64 || R == T), "a row's threads");
+    constexpr bool EARLY = V == 1;                       // the weight is asked for before the sum of squares is known (V == 2: 104 for 95 us)
     __shared__ float part[T / 64];
-    const size_t row = blockIdx.x;
-    const int K = p.a.x.K, octets = p.nb * 4;
-    float s[V > 0 ? V : 1][8];
+    const size_t row = (size_t)blockIdx.x * (T / R) + threadIdx.x / R;
+    if (row >= p.a.x.rows) return;                       // (R < T: whole groups of threads, and no barrier below)
+    const int K = p.a.x.K, octets = p.nb * 4, first = threadIdx.x % R;
+    float s[V > 0 ? V : 1][8], w[EARLY ? V : 1][8];
     float sq = 0.0f;
     auto visit = [&](float (&v)[8], int o) __attribute__((always_inline)) {
         load_sum<DT>(v, p, row, o);
@@ -128,16 +147,19 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
     };
     if constexpr (V > 0) {
 #pragma unroll
-        for (int j = 0; j < V; j++) {
-            const int o = j * T + threadIdx.x;
-            if (o < octets) visit(s[j], o);
+        for (int j = 0; j < V; j++)
+            if (j * R + first < octets) visit(s[j], j * R + first);
+        if constexpr (EARLY) {
+#pragma unroll
+            for (int j = 0; j < V; j++)
+                if (j * R + first < octets) load_weight<DT>(w[j], p, j * R + first);
         }
     } else {
-        for (int o = threadIdx.x; o < octets; o += T) visit(s[0], o);
+        for (int o = first; o < octets; o += R) visit(s[0], o);
     }
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) sq += __shfl_xor(sq, off, kWave);
-    if constexpr (T > 64) {
+    for (int off = (R < 64 ? R : 64) / 2; off >= 1; off >>= 1) sq += __shfl_xor(sq, off, kWave);
+    if constexpr (R > 64) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sq;
         __syncthreads();
         sq = 0.0f;
@@ -146,47 +168,49 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
     }
     const float r = 1.0f / sqrtf(sq / (float)K + p.a.eps);
 
-    auto finish = [&](float (&v)[8], int o) __attribute__((always_inline)) {
+    auto finish = [&](float (&v)[8], float (&g)[8], int o) __attribute__((always_inline)) {
+        if (!EARLY) load_weight<DT>(g, p, o);
         if (p.a.sum) store_octet<DT, true>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K);
-        float w[8];
-        if (!p.a.weight) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) w[i] = 1.0f;
-        } else if (p.a.weight_f32) {
-            load_octet<kF32>(w, p.a.weight, o, K);
-        } else {
-            load_octet<DT>(w, p.a.weight, o, K);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * r * w[i] : 0.0f;      // (zeros behind K whatever r is)
+        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * r * g[i] : 0.0f;      // (zeros behind K whatever r is)
         if (p.a.y) store_octet<DT, true>(v, (char *)p.a.y + row * p.a.ldy * B, o, K);
         if (p.a.q.codes) mx_store_octet<ELEM>(v, p.a.q.codes + row * p.a.q.ldc, p.a.q.scales + row * p.a.q.lds, o, p.nb, p.a.cover);
     };
     if constexpr (V > 0) {
 #pragma unroll
-        for (int j = 0; j < V; j++) {
-            const int o = j * T + threadIdx.x;
-            if (o < octets) finish(s[j], o);
-        }
+        for (int j = 0; j < V; j++)
+            if (j * R + first < octets) finish(s[j], w[EARLY ? j : 0], j * R + first);
     } else {
-        for (int o = threadIdx.x; o < octets; o += T) {
+        for (int o = first; o < octets; o += R) {
             load_sum<DT>(s[0], p, row, o);
-            finish(s[0], o);
+            finish(s[0], w[0], o);
         }
     }
 }
 
+template <int DT, int ELEM, int T, int R, int V>
+hipError_t run_norm(const NormParams &p, hipStream_t st)
+{
+    constexpr int rows = T / R;
+    rms_norm_mx_kernel<DT, ELEM, T, R, V><<<(unsigned)((p.a.x.rows + rows - 1) / rows), T, 0, st>>>(p);
+    return hipGetLastError();
+}
+
+// Rows of up to 512 values several to a workgroup (16384 x 100: 7.2 us, a workgroup of one wavefront each 16.6); as many threads as
+// leave one or two octets to each (1 x 4096 by 512 threads 3.2 us, by 256 4.1; 64 x 16384 by 1024 5.8, by 512 7.1)
 template <int DT, int ELEM>
 hipError_t run_norm(const NormParams &p, hipStream_t st)
 {
     const int octets = p.nb * 4;
-    const unsigned rows = (unsigned)p.a.x.rows;
-    if (octets <= 64) rms_norm_mx_kernel<DT, ELEM, 64, 1><<<rows, 64, 0, st>>>(p);
-    else if (octets <= 256) rms_norm_mx_kernel<DT, ELEM, 256, 1><<<rows, 256, 0, st>>>(p);
-    else if (octets <= 1024) rms_norm_mx_kernel<DT, ELEM, 256, 4><<<rows, 256, 0, st>>>(p);
-    else if (octets <= 4096) rms_norm_mx_kernel<DT, ELEM, 1024, 4><<<rows, 1024, 0, st>>>(p);
-    else rms_norm_mx_kernel<DT, ELEM, 1024, 0><<<rows, 1024, 0, st>>>(p);
-    return hipGetLastError();
+    if (octets <= 16) return run_norm<DT, ELEM, 256, 16, 1>(p, st);
+    if (octets <= 32) return run_norm<DT, ELEM, 256, 32, 1>(p, st);
+    if (octets <= 64) return run_norm<DT, ELEM, 256, 64, 1>(p, st);
+    if (octets <= 256) return run_norm<DT, ELEM, 256, 256, 1>(p, st);
+    if (octets <= 512) return run_norm<DT, ELEM, 512, 512, 1>(p, st);
+    if (octets <= 1024) return run_norm<DT, ELEM, 512, 512, 2>(p, st);
+    if (octets <= 2048) return run_norm<DT, ELEM, 1024, 1024, 2>(p, st);
+    if (octets <= 4096) return run_norm<DT, ELEM, 1024, 1024, 4>(p, st);
+    return run_norm<DT, ELEM, 1024, 1024, 0>(p, st);
 }
 
 }  // namespace
