@@ -244,37 +244,40 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     wait_loads<(NST - 2) * LPS + kFirst>();
     ring_barrier();
     if constexpr (WHOLE) {
-        // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets.
+        // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets, a few reads and loads
+        // behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step: 18 for 15 us).
         struct Set {
             Frag32<EW, EXACT> w[KK][TN];
             Frag32<EX, EXACT> x[KK][TM];
         };
         Set sets[2];
-        auto read_step = [&](Set &f, int step, int stage) __attribute__((always_inline)) {
-#pragma unroll
-            for (int kk = 0; kk < KK; kk++) {
-                const Part p = part_of(step, stage, kk);
+        auto read_part = [&](Set &f, auto part, auto group, int step, int stage) __attribute__((always_inline)) {
+            constexpr int kk = decltype(part)::value, m = decltype(group)::value;
+            const Part p = part_of(step, stage, kk);
+            if constexpr (m == 0) {
 #pragma unroll
                 for (int n = 0; n < TN; n++) read_w(f.w[kk][n], n, p);
-#pragma unroll
-                for (int m = 0; m < TM; m++) read_x(f.x[kk][m], m, p);
             }
+            read_x(f.x[kk][m], m, p);
         };
         auto do_step = [&](Set &now, Set &then, int i, int stage, int next) __attribute__((always_inline)) {
             wait_loads<(NST - 2) * LPS>();
             ring_barrier();                                            // (and every wavefront has read step i)
-            read_step(then, i + 1, next);
-            issue(i + NST, stage, None{}, std::integral_constant<int, LPS>{});
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int kk = 0; kk < KK; kk++) {
-                const Counts c = counts_of(i, kk);
-#pragma unroll
-                for (int m = 0; m < TM; m++) multiply(now.w[kk], now.x[kk][m], m, c);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            static_for<KK>([&](auto part) __attribute__((always_inline)) {
+                const Counts c = counts_of(i, decltype(part)::value);
+                static_for<TM>([&](auto group) __attribute__((always_inline)) {
+                    constexpr int kk = decltype(part)::value, m = decltype(group)::value, slot = kk * TM + m;
+                    multiply(now.w[kk], now.x[kk][m], m, c);
+                    __builtin_amdgcn_sched_barrier(0);
+                    read_part(then, part, group, i + 1, next);
+                    issue(i + NST, stage, std::integral_constant<int, slot * LPS / (KK * TM)>{}, std::integral_constant<int, (slot + 1) * LPS / (KK * TM)>{});
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
         };
-        read_step(sets[0], 0, 0);
+        static_for<KK>([&](auto part) __attribute__((always_inline)) {
+            static_for<TM>([&](auto group) __attribute__((always_inline)) { read_part(sets[0], part, group, 0, 0); });
+        });
         int stage = 0;
         for (int i = 0; i < steps; i += 2) {
             // (a step past the last multiplies zeros)
@@ -403,7 +406,7 @@ hipError_t by_shape(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 {
     switch (form) {
         case LinearMxForm::Tile64x64: return run<EX, EW, EXACT, 64, 64, 2, 2, 3, 3, true>(a, st);
-        case LinearMxForm::Tile128x128: return run<EX, EW, EXACT, 128, 128, 2, 2, 2, 2, true>(a, st);
+        case LinearMxForm::Tile128x128: return run<EX, EW, EXACT, 128, 128, 2, 2, 2, 2, !(EX == kMx4 && EW == kMx4) && !EXACT>(a, st);
         case LinearMxForm::Tile256x256: return run<EX, EW, EXACT, 256, 256, 2, 4, 2, 2, false>(a, st);
         default: return hipErrorInvalidValue;
     }
