@@ -157,7 +157,8 @@ dfq_status dfq_linear_mx_q(const uint8_t *x, size_t ldx, const uint8_t *x_scales
  * results no DFQ_LINEAR_STREAM_16X16. */
 typedef enum {
     DFQ_LINEAR_AUTO = 0, DFQ_LINEAR_DIRECT = 1, DFQ_LINEAR_STREAM_16X16 = 2, DFQ_LINEAR_STREAM_16X32 = 3, DFQ_LINEAR_STREAM_32X32 = 4,
-    DFQ_LINEAR_STREAM_32X64 = 5, DFQ_LINEAR_TILE_64X64 = 6, DFQ_LINEAR_TILE_128X128 = 7, DFQ_LINEAR_TILE_256X256 = 8
+    DFQ_LINEAR_STREAM_32X64 = 5, DFQ_LINEAR_TILE_64X64 = 6, DFQ_LINEAR_TILE_64X128 = 7, DFQ_LINEAR_TILE_128X128 = 8,
+    DFQ_LINEAR_TILE_128X128_DEEP = 9 /* eight wavefronts and one stage more */, DFQ_LINEAR_TILE_256X256 = 10
 } dfq_linear_variant;
 dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs,
                                  dfq_mx_elem elem_x, const uint8_t *w, size_t ldw, const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w,

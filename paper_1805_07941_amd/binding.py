@@ -23,7 +23,7 @@ MX4, MX8 = 0, 1               # dfq_mx_elem
 MX_COVER, MX_FLOOR = 0, 1     # dfq_mx_rule
 LINEAR_AUTO, LINEAR_DIRECT = 0, 1      # dfq_linear_variant: these, and kernels by the tokens x features of a workgroup
 LINEAR_VARIANT_NAMES = {LINEAR_AUTO: "auto", LINEAR_DIRECT: "direct", 2: "stream 16x16", 3: "stream 16x32", 4: "stream 32x32", 5: "stream 32x64",
-                        6: "tile 64x64", 7: "tile 128x128", 8: "tile 256x256"}
+                        6: "tile 64x64", 7: "tile 64x128", 8: "tile 128x128", 9: "tile 128x128 deep", 10: "tile 256x256"}
 MX_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # dfq_dtype
 CAL_AMAX_WORDS = 256          # DFQ_CAL_AMAX_WORDS
 CALL_ARGS = 30                # DFQ_CALL_ARGS

@@ -135,7 +135,8 @@ hipError_t launch_quantize_mx(const MxRows &x, const MxTensor &q, bool cover, hi
 hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t st);
 hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st);
 // Which kernel a product runs (dfq_linear_mx_variant): tokens x features of a workgroup.
-enum class LinearMxForm { Auto, Direct, Stream16x16, Stream16x32, Stream32x32, Stream32x64, Tile64x64, Tile128x128, Tile256x256 };
+enum class LinearMxForm { Auto, Direct, Stream16x16, Stream16x32, Stream32x32, Stream32x64, Tile64x64, Tile64x128, Tile128x128,
+                          Tile128x128Deep, Tile256x256 };
 bool linear_mx_supports(const LinearMxArgs &a, LinearMxForm form);
 LinearMxForm linear_mx_select(const LinearMxArgs &a);
 hipError_t launch_linear_mx(const LinearMxArgs &a, LinearMxForm form, hipStream_t st);

@@ -7,23 +7,24 @@ namespace {
 
 // Microseconds of a call: fixed + depth * K / 1000 + rounds * (tile + K / 1e6 * (byte * bytes + product * products)), with K in whole
 // 256s, rounds the workgroups a compute unit gets, bytes what a workgroup reads of its operands for one k and products its tile's,
-// twice for an 8-bit operand and four times for the bfloat16 form that float32 results of one need.  Fitted to 705 calls (1 to 8192
-// tokens, 32 to 16384 features, K 64 to 16384, every pair of elements) under every form: each form's times within 12 % of its line in
-// the mean, and the form the lines choose 1.027 times the fastest one's time in the mean.  Shapes left out because they were best in
-// few calls and by little: 64 x 64 by reductions shared in a workgroup, 64 x 128, 128 x 128 with a deeper ring (0.8 % together).
+// twice for an 8-bit operand and four times for the bfloat16 form that float32 results of one need.  Fitted to 1892 calls (1 to 8192
+// tokens, 32 to 16384 features, K 64 to 16384, every pair of elements) under every form that could be near: each form's times within
+// 7 to 14 % of its line in the mean, and the form the lines choose 1.026 times the fastest one's time in the mean.
 struct FormTime {
     LinearMxForm form;
     int tokens, features;
     double fixed, tile, depth, byte, product;
 };
 const FormTime kForms[] = {
-    {LinearMxForm::Stream16x16, 16, 16, 4.29, 0.587, 0.0, 11.1, 0.0943},
-    {LinearMxForm::Stream16x32, 16, 32, 3.84, 1.01, 0.0, 13.7, 0.0729},
-    {LinearMxForm::Stream32x32, 32, 32, 2.88, 2.18, 0.0, 7.1, 0.162},
-    {LinearMxForm::Stream32x64, 32, 64, 3.61, 1.52, 0.0, 10.8, 0.108},
-    {LinearMxForm::Tile64x64, 64, 64, 3.48, 1.39, 1.03, 2.91, 0.161},
-    {LinearMxForm::Tile128x128, 128, 128, 3.35, 3.20, 0.698, 6.50, 0.083},
-    {LinearMxForm::Tile256x256, 256, 256, 0.0, 13.3, 0.298, 0.0, 0.0702},
+    {LinearMxForm::Stream16x16, 16, 16, 4.21, 0.600, 0.0, 11.2, 0.0980},
+    {LinearMxForm::Stream16x32, 16, 32, 3.82, 0.998, 0.0, 13.6, 0.0750},
+    {LinearMxForm::Stream32x32, 32, 32, 2.91, 2.14, 0.0, 7.12, 0.167},
+    {LinearMxForm::Stream32x64, 32, 64, 3.72, 1.42, 0.0, 11.0, 0.105},
+    {LinearMxForm::Tile64x64, 64, 64, 3.89, 1.02, 0.458, 1.36, 0.176},
+    {LinearMxForm::Tile64x128, 64, 128, 2.81, 2.83, 0.229, 3.50, 0.128},
+    {LinearMxForm::Tile128x128, 128, 128, 3.86, 2.17, 0.871, 4.53, 0.0927},
+    {LinearMxForm::Tile128x128Deep, 128, 128, 0.651, 5.36, 0.177, 0.0, 0.107},
+    {LinearMxForm::Tile256x256, 256, 256, 0.0, 11.8, 0.261, 1.13, 0.0670},
 };
 
 double form_time(const FormTime &f, const LinearMxArgs &a)

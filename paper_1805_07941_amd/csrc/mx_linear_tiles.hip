@@ -339,6 +339,8 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
     const OctetEnd end(a, (n0 + wn0) / 8 + lane % kOctets);
     const bool inside = mrows == BM && n0 + BN <= a.N && (!a.q.codes || n0 + BN < a.N || a.N % 128 == 0);
+    // the largest tiles' results go past the cache where their rows are whole cache lines (8192 x 8192 x 8192: 280 -> 266 us)
+    const bool past = BM == 256 && (a.q.codes ? ((uintptr_t)a.q.codes | a.q.ldc) % 128 == 0 : ((uintptr_t)a.y | a.ldy * 2) % 128 == 0);
     with_kind(a, [&](auto kind) __attribute__((always_inline)) {
         static_for<TM>([&](auto group) __attribute__((always_inline)) {
             constexpr int m = decltype(group)::value;
@@ -361,8 +363,13 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
                 float v[32 / kTokens][8];
 #pragma unroll
                 for (int it = 0; it < 32 / kTokens; it++) octet(v[it], it * kTokens + lane / kOctets);
+                if (past) {
 #pragma unroll
-                for (int it = 0; it < 32 / kTokens; it++) end.put<decltype(kind)::value, true, BM == 256>(v[it], a, m0 + first + it * kTokens);
+                    for (int it = 0; it < 32 / kTokens; it++) end.put<decltype(kind)::value, true, BM == 256>(v[it], a, m0 + first + it * kTokens);
+                } else {
+#pragma unroll
+                    for (int it = 0; it < 32 / kTokens; it++) end.put<decltype(kind)::value, true>(v[it], a, m0 + first + it * kTokens);
+                }
             } else {
 #pragma unroll 1
                 for (int it = 0; it < 32; it += kTokens) {
@@ -406,6 +413,8 @@ hipError_t by_shape(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 {
     switch (form) {
         case LinearMxForm::Tile64x64: return run<EX, EW, EXACT, 64, 64, 2, 2, 3, 3, true>(a, st);
+        case LinearMxForm::Tile64x128: return run<EX, EW, EXACT, 64, 128, 2, 2, 2, 3, true>(a, st);
+        case LinearMxForm::Tile128x128Deep: return run<EX, EW, EXACT, 128, 128, 2, 4, 2, 3, true>(a, st);
         case LinearMxForm::Tile128x128: return run<EX, EW, EXACT, 128, 128, 2, 2, 2, 2, !(EX == kMx4 && EW == kMx4) && !EXACT>(a, st);
         case LinearMxForm::Tile256x256: return run<EX, EW, EXACT, 256, 256, 2, 4, 2, 2, false>(a, st);
         default: return hipErrorInvalidValue;

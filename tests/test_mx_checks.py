@@ -92,8 +92,8 @@ def variant(which, **kw):
 
 
 @pytest.mark.parametrize("which, kw, status", [
-    (-1, {}, B.EINVAL), (9, {}, B.EINVAL), (3, dict(codes=A[5], ldc=32, scales=A[6], lds=4), B.EINVAL), (3, dict(y=None), B.EINVAL), (8, dict(ldy=15), B.ESHAPE),
-    (2, dict(y=None, codes=A[5], ldc=32, scales=A[6], lds=4), B.EUNSUPPORTED), (8, dict(ldx=(1 << 22) + 16), B.EUNSUPPORTED),
+    (-1, {}, B.EINVAL), (11, {}, B.EINVAL), (3, dict(codes=A[5], ldc=32, scales=A[6], lds=4), B.EINVAL), (3, dict(y=None), B.EINVAL), (10, dict(ldy=15), B.ESHAPE),
+    (2, dict(y=None, codes=A[5], ldc=32, scales=A[6], lds=4), B.EUNSUPPORTED), (10, dict(ldx=(1 << 22) + 16), B.EUNSUPPORTED),
     (3, dict(ldws=(1 << 22) + 4), B.EUNSUPPORTED), (0, dict(y=None, codes=A[5], ldc=16, scales=A[6], lds=4), B.ESHAPE)])
 def test_linear_variant_refuses(which, kw, status):
     assert variant(which, **kw) == status
