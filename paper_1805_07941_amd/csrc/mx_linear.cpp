@@ -5,37 +5,45 @@ namespace dfq {
 
 namespace {
 
-// Microseconds of a call: fixed + depth * K / 1000 + rounds * (tile + K / 1e6 * (byte * bytes + product * products)), with K in whole
-// 256s, rounds the workgroups a compute unit gets, bytes what a workgroup reads of its operands for one k and products its tile's,
-// twice for an 8-bit operand and four times for the bfloat16 form that float32 results of one need.  Fitted to 1892 calls (1 to 8192
-// tokens, 32 to 16384 features, K 64 to 16384, every pair of elements) under every form that could be near: each form's times within
-// 7 to 14 % of its line in the mean, and the form the lines choose 1.026 times the fastest one's time in the mean.
+// Microseconds of a call: fixed + rounds * (tile + depth * K / 1000) + load * K / 1e6 * (byte * bytes + product * products), with K in
+// whole 256s, rounds the workgroups that a compute unit gets at most and load the same, bytes what a workgroup reads of its operands
+// for one k and products its tile's, twice for an 8-bit operand and four times for the bfloat16 form that float32 results of one need.
+// `shared`: two workgroups of a compute unit overlap, so that load is nearer to what the units get in the mean.  Fitted to 1892 calls
+// (1 to 8192 tokens, 32 to 16384 features, K 64 to 16384, every pair of elements) under every form that could be near: each form's
+// times within 7 to 14 % of its line in the mean, and the form the lines choose 1.024 times the fastest one's time in the mean (calls
+// of 8 us and more: 1.016).
 struct FormTime {
     LinearMxForm form;
     int tokens, features;
     double fixed, tile, depth, byte, product;
+    bool shared;
 };
 const FormTime kForms[] = {
-    {LinearMxForm::Stream16x16, 16, 16, 4.21, 0.600, 0.0, 11.2, 0.0980},
-    {LinearMxForm::Stream16x32, 16, 32, 3.82, 0.998, 0.0, 13.6, 0.0750},
-    {LinearMxForm::Stream32x32, 32, 32, 2.91, 2.14, 0.0, 7.12, 0.167},
-    {LinearMxForm::Stream32x64, 32, 64, 3.72, 1.42, 0.0, 11.0, 0.105},
-    {LinearMxForm::Tile64x64, 64, 64, 3.89, 1.02, 0.458, 1.36, 0.176},
-    {LinearMxForm::Tile64x128, 64, 128, 2.81, 2.83, 0.229, 3.50, 0.128},
-    {LinearMxForm::Tile128x128, 128, 128, 3.86, 2.17, 0.871, 4.53, 0.0927},
-    {LinearMxForm::Tile128x128Deep, 128, 128, 0.651, 5.36, 0.177, 0.0, 0.107},
-    {LinearMxForm::Tile256x256, 256, 256, 0.0, 11.8, 0.261, 1.13, 0.0670},
+    {LinearMxForm::Stream16x16, 16, 16, 4.21, 0.600, 0.0, 11.2, 0.0980, false},
+    {LinearMxForm::Stream16x32, 16, 32, 3.82, 0.998, 0.0, 13.6, 0.0750, false},
+    {LinearMxForm::Stream32x32, 32, 32, 2.91, 2.14, 0.0, 7.11, 0.167, false},
+    {LinearMxForm::Stream32x64, 32, 64, 3.72, 1.42, 0.0, 11.0, 0.105, false},
+    {LinearMxForm::Tile64x64, 64, 64, 4.27, 0.751, 0.262, 1.71, 0.183, false},
+    {LinearMxForm::Tile64x128, 64, 128, 2.99, 2.65, 0.446, 1.75, 0.130, false},
+    {LinearMxForm::Tile128x128, 128, 128, 4.15, 1.92, 0.370, 7.00, 0.0930, true},
+    {LinearMxForm::Tile128x128Deep, 128, 128, 0.846, 5.15, 0.270, 0.0, 0.105, false},
+    {LinearMxForm::Tile256x256, 256, 256, 0.0, 11.8, 0.638, 0.046, 0.0670, false},
 };
 
 double form_time(const FormTime &f, const LinearMxArgs &a)
 {
     const double tiles = (double)((a.M + f.tokens - 1) / f.tokens) * ((a.N + f.features - 1) / f.features);
     const double rounds = (double)(long long)((tiles + 255) / 256);
+    double load = rounds;
+    if (f.shared) {
+        load = 0.3 * rounds + 0.7 * tiles / 256;
+        if (load < 1) load = 1;
+    }
     const int bx = a.elem_x ? 8 : 4, bw = a.elem_w ? 8 : 4;
     const bool wide = bx == 8 || bw == 8, exact = wide && !a.q.codes && a.dtype == 0;
     const double bytes = (f.tokens * bx + f.features * bw) / 8.0, products = (double)f.tokens * f.features * (exact ? 4 : wide ? 2 : 1);
     const double K = (a.K + 255) / 256 * 256;
-    return f.fixed + f.depth * K * 1e-3 + rounds * (f.tile + K * 1e-6 * (f.byte * bytes + f.product * products));
+    return f.fixed + rounds * (f.tile + f.depth * K * 1e-3) + load * K * 1e-6 * (f.byte * bytes + f.product * products);
 }
 
 }  // namespace

@@ -7,8 +7,9 @@
 // read only, and reads the next 64 values' operands while the matrix pipe is busy with these.
 //
 // Scales come in chunks of 16 bytes of a row (512 values): a row's four bytes of one step would cost as many cache lines as its 128
-// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c, into a ring of its own.  What lies behind a row's last block is masked twice: codes by an offset past the buffer (zeros arrive), scales by a
-// comparison when they are read, so that neither the next row's bytes nor padding count.
+// bytes of codes.  Chunk c + 1 is loaded in equal parts with the steps of chunk c, into a ring of its own.  What lies behind a row's
+// last block is masked twice: codes by an offset past the buffer (zeros arrive), scales by a comparison when they are read, so that
+// neither the next row's bytes nor padding count.
 #include "conv_ring.hpp"
 #include "mx_linear.hpp"
 
@@ -245,7 +246,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     ring_barrier();
     if constexpr (WHOLE) {
         // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets, a few reads and loads
-        // behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step: 18 for 15 us).
+        // behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step: 256 x 4096 x 4096 on 8 by 4 bits 14.1 for 12.9 us).
         struct Set {
             Frag32<EW, EXACT> w[KK][TN];
             Frag32<EX, EXACT> x[KK][TM];
