@@ -1149,11 +1149,11 @@ dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, s
     if (!M) return DFQ_OK;
     if (!elem_ok(elem_x) || !elem_ok(elem_w) || (y && codes)) return DFQ_EINVAL;
     DFQ_TRY(check_size(M, K));
+    DFQ_TRY(check_size(M, N));
     DFQ_TRY(check_mx_rows(x, ldx, x_scales, ldxs, elem_x, K));
     DFQ_TRY(check_mx_rows(w, ldw, w_scales, ldws, elem_w, K));
     if ((uintptr_t)bias % 4) return DFQ_EINVAL;
     if (codes) {
-        DFQ_TRY(check_size(M, N));
         DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, N));
     } else {
         DFQ_TRY(check_float_rows(y, ldy, dtype, N));
@@ -1217,7 +1217,6 @@ dfq_status dfq_rms_norm_mx(const void *x, size_t ldx, const void *add, size_t ld
 extern "C" {
 
 // ---- a pass as one call
-
 
 }  // extern "C"
 

@@ -73,7 +73,7 @@ SHARED = [(dict(x=None), B.EINVAL), (dict(xs=None), B.EINVAL), (dict(w=None), B.
 
 @pytest.mark.parametrize("kw, status", SHARED + [
     (dict(y=None), B.EINVAL), (dict(y=A[4] + 1), B.EINVAL), (dict(dtype=4), B.EINVAL), (dict(ldy=15), B.ESHAPE), (dict(y=A[0] + 2), B.EINVAL), (dict(y=A[3]), B.EINVAL),
-    (dict(bias=A[7], y=A[7] + 60), B.EINVAL)])
+    (dict(bias=A[7], y=A[7] + 60), B.EINVAL), (dict(N=BIG + 1, ldy=2 * BIG), B.EUNSUPPORTED), (dict(N=0x7fffffff, ldy=1 << 31), B.EUNSUPPORTED)])
 def test_linear_refuses(kw, status):
     assert linear(**kw) == status
 
