@@ -243,6 +243,8 @@ class CallList:
             if number is None:
                 number = self._numbers[name] = lib().dfq_call_number(name.encode())
             words.append((number & 0xffffffff) | len(args) << 32)
+            if C.c_float in fn.argtypes:
+                args = [float(a) if t is C.c_float else a for a, t in zip(args, fn.argtypes)]
             words += [a if type(a) is int else a.frac if type(a) is Fmt else 0 if a is None else of_array(a) if isinstance(a, C.Array) else
                       struct.unpack("<I", struct.pack("<f", a))[0] if type(a) is float else int(a) for a in args]
             words += _ZEROS[len(args):]

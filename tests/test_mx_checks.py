@@ -131,6 +131,16 @@ def test_records_of_the_calls():
         assert e.value.status == status
 
 
+def test_a_record_of_a_whole_number_where_a_float_belongs():
+    """0x7f800000 as a float's bits would be an infinity and refused; as a number it is an eps like any other."""
+    fn = B.lib().dfq_rms_norm_mx
+    args = (A[0], 63, None, 0, None, 0, 1, None, 1, 0x7f800000, A[4], 64, None, 0, None, 0, 1, 0, 3, 64)
+    assert fn(*args, None) == B.ESHAPE
+    with pytest.raises(B.DfqError) as e:
+        B.CallList([(fn, args)]).run(None)
+    assert e.value.status == B.ESHAPE
+
+
 def test_tensors_on_the_host_are_refused():
     x = torch.zeros(2, 64)
     q = B.MxTensor.empty(2, 64, B.MX8, "cpu")
