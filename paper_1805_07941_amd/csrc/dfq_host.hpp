@@ -85,6 +85,9 @@ struct CalConcat {
     int32_t *frac_out = nullptr;
 };
 
+// threads of a launch along an axis of its grid: the hardware counts them in 32 bits
+constexpr unsigned kMostThreads = 0xffffffffu;
+
 // Rows of floating-point values: `ld` elements apart, K of them, dtype one of dfq_dtype.
 struct MxRows {
     const void *p;

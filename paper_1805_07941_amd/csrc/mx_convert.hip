@@ -99,6 +99,7 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 struct NormParams {
     RmsNormArgs a;
     int nb;
+    size_t row0;             // the launch's first row
 };
 
 template <int DT>
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
     static_assert(R <= T && (R <= 64 || R == T), "a row's threads");
     constexpr bool EARLY = V == 1;                       // the weight is asked for before the sum of squares is known (V == 2: 104 for 95 us)
     __shared__ float part[T / 64];
-    const size_t row = (size_t)blockIdx.x * (T / R) + threadIdx.x / R;
+    const size_t row = p.row0 + (size_t)blockIdx.x * (T / R) + threadIdx.x / R;
     if (row >= p.a.x.rows) return;                       // (R < T: whole groups of threads, and no barrier below)
     const int K = p.a.x.K, octets = p.nb * 4, first = threadIdx.x % R;
     float s[V > 0 ? V : 1][8], w[EARLY ? V : 1][8];
@@ -189,10 +190,13 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
 }
 
 template <int DT, int ELEM, int T, int R, int V>
-hipError_t run_norm(const NormParams &p, hipStream_t st)
+hipError_t run_norm(NormParams p, hipStream_t st)
 {
-    constexpr int rows = T / R;
-    rms_norm_mx_kernel<DT, ELEM, T, R, V><<<(unsigned)((p.a.x.rows + rows - 1) / rows), T, 0, st>>>(p);
+    constexpr size_t rows = T / R, most = kMostThreads / T * rows;
+    for (; p.row0 < p.a.x.rows; p.row0 += most) {
+        const size_t n = p.a.x.rows - p.row0 < most ? p.a.x.rows - p.row0 : most;
+        rms_norm_mx_kernel<DT, ELEM, T, R, V><<<(unsigned)((n + rows - 1) / rows), T, 0, st>>>(p);
+    }
     return hipGetLastError();
 }
 
@@ -227,7 +231,7 @@ hipError_t launch_dequantize_mx(const MxTensor &q, const MxRows &x, hipStream_t 
 
 hipError_t launch_rms_norm_mx(const RmsNormArgs &a, hipStream_t st)
 {
-    const NormParams p{a, (a.x.K + kMxBlock - 1) / kMxBlock};
+    const NormParams p{a, (a.x.K + kMxBlock - 1) / kMxBlock, 0};
     const bool mx8 = a.q.elem == kMx8;
     if (a.x.dtype == kF32) return mx8 ? run_norm<kF32, kMx8>(p, st) : run_norm<kF32, kMx4>(p, st);
     if (a.x.dtype == kBF16) return mx8 ? run_norm<kBF16, kMx8>(p, st) : run_norm<kBF16, kMx4>(p, st);

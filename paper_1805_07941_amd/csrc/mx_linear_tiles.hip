@@ -245,8 +245,9 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     wait_loads<(NST - 2) * LPS + kFirst>();
     ring_barrier();
     if constexpr (WHOLE) {
-        // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets, a few reads and loads
-        // behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step: 256 x 4096 x 4096 on 8 by 4 bits 14.1 for 12.9 us).
+        // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets, a few reads and
+        // loads behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step:
+        // 256 x 4096 x 4096 on 8 by 4 bits 14.1 for 12.9 us).
         struct Set {
             Frag32<EW, EXACT> w[KK][TN];
             Frag32<EX, EXACT> x[KK][TM];
@@ -397,8 +398,7 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
     TileParams p{a, (a.K + kMxBlock - 1) / kMxBlock};
     p.steps = (a.K + KS - 1) / KS;
     p.tiles_n = (a.N + BN - 1) / BN;
-    // token rows of one launch: 2^31 tiles at most
-    const size_t most = (size_t)(0x7fffffff / p.tiles_n) * BM;
+    const size_t most = (size_t)(kMostThreads / (WM * WN * 64) / p.tiles_n) * BM;     // token rows of one launch
     for (size_t m = 0; m < a.M; m += most) {
         p.a = a;
         advance_tokens(p.a, m);

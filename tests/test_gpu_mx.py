@@ -507,3 +507,32 @@ def test_tensors_of_more_dimensions_and_refusals(B):
     empty = B.quantize_mx(x[:0].view(0, 96))
     assert B.linear_mx(empty, w).shape == (0, 40) and B.dequantize_mx(empty).shape == (0, 96) and B.linear_mx_q(empty, w).codes.shape == (0, 64)
     assert B.rms_norm_mx(x[:0].view(0, 96))[0].codes.shape == (0, 96)
+
+
+def test_norm_of_more_rows_than_one_grid_holds(B):
+    """2^28 + 37 rows of one value, 16 threads to a row: the threads no longer fit 32 bits.  x / |x| of +-2 is exact."""
+    rows = (1 << 28) + 37
+    x = (torch.randint(0, 2, (rows, 1), device=DEV, dtype=torch.int8) * 4 - 2).bfloat16()
+    q, y, _ = B.rms_norm_mx(x, eps=0.0, elem=B.MX4, want_y=True)
+    assert torch.equal(y, x * 0.5)
+    want = B.quantize_mx(torch.tensor([[1.0], [-1.0]], device=DEV), B.MX4)
+    for first in range(0, rows, 1 << 26):
+        part = slice(first, first + (1 << 26))
+        negative = x[part] < 0
+        assert torch.equal(q.codes[part, :1], torch.where(negative, want.codes[1, 0], want.codes[0, 0])) and not q.codes[part, 1:].any()
+        assert torch.equal(q.scales[part, 0], want.scales[0, 0].expand(negative.shape[0])) and not q.scales[part, 1:].any()
+
+
+@pytest.mark.parametrize("variant", [2, 6, 10])
+def test_linear_of_more_tokens_than_one_grid_holds(B, variant):
+    """2^30 + 5 tokens: 2^24 tiles of 256 threads and more.  The first value of each token times 1."""
+    M = (1 << 30) + 5
+    x = B.MxTensor(torch.randint(0, 256, (M, 16), device=DEV, dtype=torch.uint8), torch.full((M, 4), 128, device=DEV, dtype=torch.uint8), B.MX4, 32)
+    w = B.quantize_mx(torch.eye(1, 32, device=DEV), B.MX4)
+    y = torch.full((M, 1), 77.0, device=DEV, dtype=torch.bfloat16)
+    B.linear_mx(x, w, out=y, dtype=torch.bfloat16, variant=variant)
+    magnitude = mx.magnitudes(mx.MX4)
+    table = torch.tensor(np.concatenate((magnitude, -magnitude)) * 2, device=DEV, dtype=torch.bfloat16)
+    step = 1 << 26
+    for first in range(0, M, step):
+        assert torch.equal(y[first:first + step, 0], table[(x.codes[first:first + step, 0] & 15).int()])
