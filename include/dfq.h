@@ -169,7 +169,8 @@ dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, s
  *   s = x + add;  v = s / sqrt(mean(s^2) + eps) * weight;  sum = s rounded to dtype;  y = v rounded to dtype;  codes, scales = v converted
  * add, sum, weight (NULL: ones), y and codes may be NULL, y and codes not both; the norm reads s unrounded.  x, add, sum and y are rows
  * of dtype, weight K values of wtype, which is dtype or DFQ_F32.  sum may be x or add (same address and row distance): the residual
- * stream is then updated in place.  eps >= 0 and finite; a row of zeros with eps = 0 is NaN. */
+ * stream is then updated in place.  eps >= 0 and finite; a row of zeros with eps = 0 is NaN.  Squares outside float32's range do not
+ * spoil a row whose values are inside it. */
 dfq_status dfq_rms_norm_mx(const void *x, size_t ldx, const void *add, size_t ldadd, void *sum, size_t ldsum, dfq_dtype dtype,
                            const void *weight, dfq_dtype wtype, float eps, void *y, size_t ldy, uint8_t *codes, size_t ldc, uint8_t *scales,
                            size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t rows, int K, dfq_stream stream);

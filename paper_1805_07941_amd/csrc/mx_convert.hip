@@ -1,6 +1,8 @@
 // Conversion of float rows to microscaled ones and back, and the root-mean-square norm whose result is converted on the way out.
 // All three move bytes: a lane takes eight values (16 bytes of a 16-bit type), the four lanes of a quad a block of 32, whose largest
 // magnitude is found by two lane exchanges inside the quad.
+#include <type_traits>
+
 #include "dfq_host.hpp"
 #include "mx_device.hpp"
 #include "conv_epilogue.hpp"
@@ -92,9 +94,11 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 }
 
 // ---- root-mean-square norm: s = x + add, y = s / sqrt(mean(s^2) + eps) * weight.
-// R threads to a row (a wavefront's part, a wavefront or a workgroup), V octets of the sum held in registers between the two passes over it; V == 0: rows too long for that, the second pass reads x and add again.  Bound by the bytes: x and add
-// read, the sum and the codes written (8192 x 8192 bfloat16 to 8 bits, 473 MB: 95 us, 5.0 TB/s; a copy of that size 5.1 to 5.3).
-// The sum goes past the cache; the codes stay, the product behind the norm reads them: 8192 x 8192 codes past it 78 us, but norm and
+// R threads to a row (a wavefront's part, a wavefront or a workgroup), V octets of the sum held in registers between the two passes
+// over it; V == 0: rows too long for that, the second pass reads x and add again.  Bound by the bytes: x and add read, the sum and the
+// codes written (8192 x 8192 bfloat16 to 8 bits, 473 MB: 93 us, 5.1 TB/s; a copy of that size 5.1 to 5.3).  The sum of squares is a
+// float32 one (in 64 bits 8192 x 8192 took 104 us).  Squares that leave float32's range (rows around 2^50 and above, 2^-40 and below)
+// are added again, of values times a power of two.  The sum goes past the cache; the codes stay, the product behind the norm reads them: 8192 x 8192 codes past it 78 us, but norm and
 // product 518 for 509, 16384 x 4096 with its product 314 for 295.
 struct NormParams {
     RmsNormArgs a;
@@ -140,40 +144,55 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
     if (row >= p.a.x.rows) return;                       // (R < T: whole groups of threads, and no barrier below)
     const int K = p.a.x.K, octets = p.nb * 4, first = threadIdx.x % R;
     float s[V > 0 ? V : 1][8], w[EARLY ? V : 1][8];
-    float sq = 0.0f;
-    auto visit = [&](float (&v)[8], int o) __attribute__((always_inline)) {
-        load_sum<DT>(v, p, row, o);
+    // the sum of the squares of the row's values times c
+    auto squares = [&](float c, auto again) __attribute__((always_inline)) {
+        float sq = 0.0f;
+        auto visit = [&](const float (&v)[8]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) sq += v[i] * v[i];
-    };
-    if constexpr (V > 0) {
-#pragma unroll
-        for (int j = 0; j < V; j++)
-            if (j * R + first < octets) visit(s[j], j * R + first);
-        if constexpr (EARLY) {
+            for (int i = 0; i < 8; i++) sq += (v[i] * c) * (v[i] * c);
+        };
+        if constexpr (V > 0) {
 #pragma unroll
             for (int j = 0; j < V; j++)
-                if (j * R + first < octets) load_weight<DT>(w[j], p, j * R + first);
+                if (j * R + first < octets) {
+                    if constexpr (!decltype(again)::value) load_sum<DT>(s[j], p, row, j * R + first);
+                    visit(s[j]);
+                }
+            if constexpr (EARLY && !decltype(again)::value) {
+#pragma unroll
+                for (int j = 0; j < V; j++)
+                    if (j * R + first < octets) load_weight<DT>(w[j], p, j * R + first);
+            }
+        } else {
+            for (int o = first; o < octets; o += R) {
+                load_sum<DT>(s[0], p, row, o);
+                visit(s[0]);
+            }
         }
-    } else {
-        for (int o = first; o < octets; o += R) visit(s[0], o);
-    }
 #pragma unroll
-    for (int off = (R < 64 ? R : 64) / 2; off >= 1; off >>= 1) sq += __shfl_xor(sq, off, kWave);
-    if constexpr (R > 64) {
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sq;
-        __syncthreads();
-        sq = 0.0f;
+        for (int off = (R < 64 ? R : 64) / 2; off >= 1; off >>= 1) sq += __shfl_xor(sq, off, kWave);
+        if constexpr (R > 64) {
+            if constexpr (decltype(again)::value) __syncthreads();
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sq;
+            __syncthreads();
+            sq = 0.0f;
 #pragma unroll
-        for (int i = 0; i < T / 64; i++) sq += part[i];
+            for (int i = 0; i < T / 64; i++) sq += part[i];
+        }
+        return sq;
+    };
+    float c = 1.0f, sq = squares(1.0f, std::false_type{}), mean = sq / (float)K + p.a.eps;
+    if (!(sq <= 0x1p100f) || mean < 0x1p-80f) {          // (the same for all of a row's threads)
+        c = sq <= 0x1p100f ? 0x1p90f : 0x1p-76f;       // (2^22 squares of up to 2^128 or down to 2^-149 stay normal)
+        mean = squares(c, std::true_type{}) / (float)K + p.a.eps * c * c;
     }
-    const float r = 1.0f / sqrtf(sq / (float)K + p.a.eps);
+    const float r = 1.0f / sqrtf(mean);
 
     auto finish = [&](float (&v)[8], float (&g)[8], int o) __attribute__((always_inline)) {
         if (!EARLY) load_weight<DT>(g, p, o);
         if (p.a.sum) store_octet<DT, true>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K);
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * r * g[i] : 0.0f;      // (zeros behind K whatever r is)
+        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * c * r * g[i] : 0.0f;      // (zeros behind K whatever r is)
         if (p.a.y) store_octet<DT, true>(v, (char *)p.a.y + row * p.a.ldy * B, o, K);
         if (p.a.q.codes) mx_store_octet<ELEM>(v, p.a.q.codes + row * p.a.q.ldc, p.a.q.scales + row * p.a.q.lds, o, p.nb, p.a.cover);
     };

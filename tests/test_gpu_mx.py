@@ -536,3 +536,23 @@ def test_linear_of_more_tokens_than_one_grid_holds(B, variant):
     step = 1 << 26
     for first in range(0, M, step):
         assert torch.equal(y[first:first + step, 0], table[(x.codes[first:first + step, 0] & 15).int()])
+
+
+@pytest.mark.parametrize("K", [1, 20, 512, 3001, 8192, 16384, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rms_norm_of_rows_whose_squares_leave_the_range(B, dtype, K):
+    """Rows from float32's smallest values to its largest ones, several of them to a wavefront; 1e-30 and 0 for eps."""
+    rng = rng_of("range", dtype, K)
+    powers = (-146, -130, -126, -100, -64, -45, -41, -40, -39, 0, 40, 49, 50, 51, 64, 100, 120, 126)
+    x = torch.from_numpy(np.clip(rng.standard_normal((len(powers), K)), -1.9, 1.9) * np.exp2(np.array(powers, np.float64))[:, None]).to(TYPES[dtype])
+    x[:, 0] = torch.from_numpy(np.exp2(np.array(powers, np.float64))).to(TYPES[dtype])      # (a row of zeros: 2^-146 in bfloat16, NaN with eps = 0)
+    for eps in (0.0, 1e-30):
+        with np.errstate(invalid="ignore"):
+            _, v = mx.rms_norm(x.float().numpy(), None, None, eps)
+        q, y, _ = B.rms_norm_mx(x.to(DEV), None, eps, want_y=True)
+        err = NORM_U * np.abs(v)
+        tol = err + HALF[dtype] * (np.abs(v) + err) + 2.0 ** (-150 if dtype == "f32" else -134)
+        assert ((np.abs(host(y) - v) <= tol) | np.isnan(host(y)) & np.isnan(v)).all()
+        same = B.quantize_mx(y.float())
+        if dtype == "f32":
+            assert torch.equal(q.codes, same.codes) and torch.equal(q.scales, same.scales)
