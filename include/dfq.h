@@ -117,7 +117,9 @@ dfq_status dfq_dequantize_np(const uint8_t *codes, float *x, size_t n, int nbits
  * aligned, ldc a multiple of 16 and at least that many.  Its scales start at scales + r * lds; scales 4-byte aligned, lds a
  * multiple of 4 and at least ceil(K / 32); the bytes from there to the next multiple of 4 are padding, written as zeros and read
  * without effect.  Floating-point rows are `ld` ELEMENTS of `dtype` apart, ld >= K, aligned to their type.  Every call takes rows of
- * up to 2^22 values and up to 2^31 - 1 rows (DFQ_EUNSUPPORTED beyond); rows == 0 (M == 0) is a no-op.  Everything DEVICE.
+ * up to 2^22 values and up to 2^31 - 1 rows, 2^40 apart at most and 2^48 from first to last (DFQ_EUNSUPPORTED beyond); rows == 0
+ * (M == 0) is a no-op.  What is written lies, from its first row to its last, apart from everything else of the call (DFQ_EINVAL), but
+ * for the sums in place of dfq_rms_norm_mx.  Everything DEVICE.
  *
  * The exponent e = s - 127 of a block with largest magnitude amax, top the largest element (6 or 448):
  *   DFQ_MX_COVER  the smallest e with amax <= top * 2^e (the rule of dfq_fmt_from_absmax_f32: the largest value is never clipped)

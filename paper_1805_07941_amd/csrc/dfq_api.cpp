@@ -1065,7 +1065,8 @@ inline size_t dtype_size(dfq_dtype t) { return t == DFQ_F32 ? 4 : 2; }
 
 constexpr int kMostMxValues = 1 << 22;
 constexpr size_t kMostMxRows = 0x7fffffff;
-constexpr size_t kMostMxDistance = (size_t)1 << 40;      // bytes between rows: products with a number of rows stay in 64 bits
+// bytes or elements between rows, and from the first row to the last: addresses stay in 64 bits
+constexpr size_t kMostMxDistance = (size_t)1 << 40, kMostMxReach = (size_t)1 << 48;
 
 inline size_t mx_row_bytes(dfq_mx_elem e, int K) { return (size_t)((K + 31) / 32) * (e == DFQ_MX8 ? 32 : 16); }
 
@@ -1075,18 +1076,20 @@ dfq_status check_size(size_t rows, int K)
     return K > kMostMxValues || rows > kMostMxRows ? DFQ_EUNSUPPORTED : DFQ_OK;
 }
 
-dfq_status check_float_rows(const void *p, size_t ld, dfq_dtype t, int K)
+inline bool too_far(size_t ld, size_t rows) { return ld > kMostMxDistance || ld > kMostMxReach / rows; }
+
+dfq_status check_float_rows(const void *p, size_t ld, dfq_dtype t, size_t rows, int K)
 {
     if (!p || (uintptr_t)p % dtype_size(t)) return DFQ_EINVAL;
     if (ld < (size_t)K) return DFQ_ESHAPE;
-    return ld > kMostMxDistance ? DFQ_EUNSUPPORTED : DFQ_OK;
+    return too_far(ld, rows) ? DFQ_EUNSUPPORTED : DFQ_OK;
 }
 
-dfq_status check_mx_rows(const uint8_t *codes, size_t ldc, const uint8_t *scales, size_t lds, dfq_mx_elem e, int K)
+dfq_status check_mx_rows(const uint8_t *codes, size_t ldc, const uint8_t *scales, size_t lds, dfq_mx_elem e, size_t rows, int K)
 {
     if (!codes || !scales || (uintptr_t)codes % 16 || (uintptr_t)scales % 4) return DFQ_EINVAL;
     if (ldc % 16 || lds % 4 || ldc < mx_row_bytes(e, K) || lds < (size_t)((K + 31) / 32)) return DFQ_ESHAPE;
-    return ldc > kMostMxDistance || lds > kMostMxDistance ? DFQ_EUNSUPPORTED : DFQ_OK;
+    return too_far(ldc, rows) || too_far(lds, rows) ? DFQ_EUNSUPPORTED : DFQ_OK;
 }
 
 inline Span float_span(const void *p, size_t ld, dfq_dtype t, size_t rows, int K)
@@ -1118,8 +1121,8 @@ dfq_status dfq_quantize_mx(const void *x, size_t ldx, dfq_dtype dtype, size_t ro
     if (!dtype_ok(dtype) || !elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
     DFQ_TRY(check_size(rows, K));
     if (!rows) return DFQ_OK;
-    DFQ_TRY(check_float_rows(x, ldx, dtype, K));
-    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, K));
+    DFQ_TRY(check_float_rows(x, ldx, dtype, rows, K));
+    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, rows, K));
     if (!apart({float_span(x, ldx, dtype, rows, K)}, {codes_span(codes, ldc, elem, rows, K), scales_span(scales, lds, rows, K)})) return DFQ_EINVAL;
     return from_hip(launch_quantize_mx(MxRows{x, ldx, rows, K, dtype}, MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, (hipStream_t)stream));
 }
@@ -1130,8 +1133,8 @@ dfq_status dfq_dequantize_mx(const uint8_t *codes, size_t ldc, const uint8_t *sc
     if (!dtype_ok(dtype) || !elem_ok(elem)) return DFQ_EINVAL;
     DFQ_TRY(check_size(rows, K));
     if (!rows) return DFQ_OK;
-    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, K));
-    DFQ_TRY(check_float_rows(x, ldx, dtype, K));
+    DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, rows, K));
+    DFQ_TRY(check_float_rows(x, ldx, dtype, rows, K));
     if (!apart({codes_span(codes, ldc, elem, rows, K), scales_span(scales, lds, rows, K)}, {float_span(x, ldx, dtype, rows, K)})) return DFQ_EINVAL;
     return from_hip(launch_dequantize_mx(MxTensor{const_cast<uint8_t *>(codes), ldc, const_cast<uint8_t *>(scales), lds, elem}, MxRows{x, ldx, rows, K, dtype},
                                          (hipStream_t)stream));
@@ -1150,13 +1153,13 @@ dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, s
     if (!elem_ok(elem_x) || !elem_ok(elem_w) || (y && codes)) return DFQ_EINVAL;
     DFQ_TRY(check_size(M, K));
     DFQ_TRY(check_size(M, N));
-    DFQ_TRY(check_mx_rows(x, ldx, x_scales, ldxs, elem_x, K));
-    DFQ_TRY(check_mx_rows(w, ldw, w_scales, ldws, elem_w, K));
+    DFQ_TRY(check_mx_rows(x, ldx, x_scales, ldxs, elem_x, M, K));
+    DFQ_TRY(check_mx_rows(w, ldw, w_scales, ldws, elem_w, (size_t)N, K));
     if ((uintptr_t)bias % 4) return DFQ_EINVAL;
     if (codes) {
-        DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, N));
+        DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, M, N));
     } else {
-        DFQ_TRY(check_float_rows(y, ldy, dtype, N));
+        DFQ_TRY(check_float_rows(y, ldy, dtype, M, N));
     }
     if (!apart({codes_span(x, ldx, elem_x, M, K), scales_span(x_scales, ldxs, M, K), codes_span(w, ldw, elem_w, N, K), scales_span(w_scales, ldws, N, K),
                 {bias, (size_t)N * 4}},
@@ -1193,11 +1196,11 @@ dfq_status dfq_rms_norm_mx(const void *x, size_t ldx, const void *add, size_t ld
     DFQ_TRY(check_size(rows, K));
     if (!rows) return DFQ_OK;
     if (!y && !codes) return DFQ_EINVAL;
-    DFQ_TRY(check_float_rows(x, ldx, dtype, K));
-    if (add) DFQ_TRY(check_float_rows(add, ldadd, dtype, K));
-    if (sum) DFQ_TRY(check_float_rows(sum, ldsum, dtype, K));
-    if (y) DFQ_TRY(check_float_rows(y, ldy, dtype, K));
-    if (codes) DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, K));
+    DFQ_TRY(check_float_rows(x, ldx, dtype, rows, K));
+    if (add) DFQ_TRY(check_float_rows(add, ldadd, dtype, rows, K));
+    if (sum) DFQ_TRY(check_float_rows(sum, ldsum, dtype, rows, K));
+    if (y) DFQ_TRY(check_float_rows(y, ldy, dtype, rows, K));
+    if (codes) DFQ_TRY(check_mx_rows(codes, ldc, scales, lds, elem, rows, K));
     if ((uintptr_t)weight % dtype_size(wtype)) return DFQ_EINVAL;
     // in place: a row of the sum is written where the same row was read
     const Span xs = float_span(x, ldx, dtype, rows, K), as = float_span(add, ldadd, dtype, rows, K), ws = {weight, weight ? K * dtype_size(wtype) : 0};

@@ -110,6 +110,15 @@ def test_norm_refuses(kw, status):
     assert norm(**kw) == status
 
 
+@pytest.mark.parametrize("call, kw", [
+    (quantize, dict(ldx=1 << 40)), (quantize, dict(ldc=1 << 40)), (quantize, dict(lds=1 << 40)), (dequantize, dict(ldx=1 << 40)), (linear, dict(ldx=1 << 40)),
+    (linear, dict(ldy=1 << 40)), (linear_q, dict(ldc=1 << 40)), (norm, dict(ldadd=1 << 40)), (norm, dict(ldsum=1 << 40)), (norm, dict(ldy=1 << 40))])
+def test_rows_whose_addresses_leave_64_bits(call, kw):
+    """2^24 + 1 of them 2^40 apart: a distance that wraps around is no check of what lies where."""
+    rows = "M" if call in (linear, linear_q) else "rows"
+    assert call(**kw, **{rows: (1 << 24) + 1}) == B.EUNSUPPORTED
+
+
 def test_nothing_to_do():
     assert quantize(rows=0, x=None, codes=None, scales=None) == B.OK and dequantize(rows=0, x=None) == B.OK
     assert linear(M=0, x=None, y=None) == B.OK and linear_q(M=0, codes=None) == B.OK and norm(rows=0, x=None, y=None, codes=None) == B.OK
