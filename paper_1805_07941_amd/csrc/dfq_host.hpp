@@ -2,6 +2,7 @@
 // kernel family.  Launchers assume validated arguments and only enqueue work.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <atomic>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -87,6 +88,18 @@ struct CalConcat {
 
 // threads of a launch along an axis of its grid: the hardware counts them in 32 bits
 constexpr unsigned kMostThreads = 0xffffffffu;
+
+// Lets a kernel have more dynamic LDS than the default, once for each device (`devices`: the kernel's own, a bit to each).
+inline hipError_t allow_lds(const void *kernel, int bytes, std::atomic<unsigned long long> &devices)
+{
+    int d = 0;
+    hipError_t e = hipGetDevice(&d);
+    const unsigned long long bit = 1ull << (d & 63);
+    if (e != hipSuccess || devices.load(std::memory_order_relaxed) & bit) return e;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // Rows of floating-point values: `ld` elements apart, K of them, dtype one of dfq_dtype.
 struct MxRows {

@@ -146,7 +146,8 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
     constexpr int kLds = NW * NST * (FT * 16 * StreamRow<EW>::kBytes + TT * 16 * StreamRow<EX>::kBytes + ((FT + 1) / 2 + (TT + 1) / 2) * 256);
     static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
     const auto kernel = linear_mx_stream_kernel<EX, EW, EXACT, FT, TT, NW, NST>;
-    static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    static std::atomic<unsigned long long> devices{0};
+    const hipError_t allowed = allow_lds((const void *)kernel, kLds, devices);
     if (allowed != hipSuccess) return allowed;
     const size_t most = (size_t)65535 * TT * 16;         // rows of the grid
     for (size_t m = 0; m < a.M; m += most) {

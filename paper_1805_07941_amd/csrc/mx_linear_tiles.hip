@@ -393,7 +393,8 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
     constexpr int kLds = NST * (BM * Operand<EX, KS>::kRow + BN * Operand<EW, KS>::kRow) + scale_chunks(NST, 512 / KS) * (((BM + BN) / 16 + kParts - 1) / kParts * kParts * 256);
     static_assert(kLds <= kLdsBytes, "LDS of a compute unit");
     const auto kernel = linear_mx_tiles_kernel<EX, EW, EXACT, BM, BN, WM, WN, OCC, NST, WHOLE>;
-    static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    static std::atomic<unsigned long long> devices{0};
+    const hipError_t allowed = allow_lds((const void *)kernel, kLds, devices);
     if (allowed != hipSuccess) return allowed;
     TileParams p{a, (a.K + kMxBlock - 1) / kMxBlock};
     p.steps = (a.K + KS - 1) / KS;
