@@ -52,8 +52,8 @@ constexpr int scale_chunks(int nst, int spc) { return (nst + spc - 1) / spc + 2 
 __device__ __forceinline__ int scale_key(int row) { return (row >> 3) & 3; }
 
 // One lane's operands of a 32-row group for 64 values: what v_mfma_scale_f32_32x32x64_f8f6f4 wants (with h = lane / 32: of 4-bit
-// elements block h, of 8-bit ones bytes 16h.. of both blocks), and block h's scale byte.  EXACT: bytes 16h.. (4 bits: 8h..) of both
-// blocks, and both scales.
+// elements block h, of 8-bit ones bytes 16h.. of both blocks).  EXACT: bytes 16h.. (4 bits: 8h..) of both blocks, and both scales.
+// (Otherwise scales are words, the bytes of four blocks, shifted so that block h's is the lowest: two parts take its bytes 0 and 2.)
 template <int ELEM, bool EXACT>
 struct Frag32 {
     v4i lo, hi;
@@ -138,13 +138,15 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     auto issue = [&](int step, int stage, auto from, auto to) __attribute__((always_inline)) {
         constexpr int kFrom = decltype(from)::value, kTo = decltype(to)::value;
         const unsigned base = (unsigned)__builtin_amdgcn_readfirstlane((int)(lds_base + (unsigned)stage * kStage + (unsigned)wave * 1024u));
-        const unsigned kx = (unsigned)step * OX::kRow, kw = (unsigned)step * OW::kRow;
-        const unsigned badx = kx + xp < xrow ? 0u : kOutOfRange, badw = kw + wp < wrow ? 0u : kOutOfRange;
+        // (offsets stay below 2^31: out of range is a bit more to add)
+        unsigned kx = (unsigned)step * OX::kRow, kw = (unsigned)step * OW::kRow;
+        kx += kx + xp < xrow ? 0u : kOutOfRange;
+        kw += kw + wp < wrow ? 0u : kOutOfRange;
 #pragma unroll
         for (int q = kFrom; q < kTo; q++) {
             const int j = q < XL ? q : q < XL + WL ? q - XL : q - XL - WL;
-            if (q < XL) load_piece_to_lds((xoff + (kx + j * (XR * NW) * ldx)) | badx, xr, base + (unsigned)j * (NW * 1024u));
-            else if (q < XL + WL) load_piece_to_lds((woff + (kw + j * (WR * NW) * ldw)) | badw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
+            if (q < XL) load_piece_to_lds(xoff + j * (XR * NW) * ldx + kx, xr, base + (unsigned)j * (NW * 1024u));
+            else if (q < XL + WL) load_piece_to_lds(woff + j * (WR * NW) * ldw + kw, wr, base + (unsigned)(BM * OX::kRow) + (unsigned)j * (NW * 1024u));
             else issue_scales(step % SPC * SL + j, step / SPC + 1);
         }
     };
@@ -181,8 +183,6 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
         if constexpr (EXACT) {
             f.scale = *(const unsigned char *)(lds + scale_at);
             f.scale1 = *(const unsigned char *)(lds + scale_at + 1);
-        } else {
-            f.scale = *(const unsigned char *)(lds + scale_at + h);
         }
     };
     // 64 values of the reduction axis: part kk of a step
@@ -200,6 +200,8 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     auto read_x = [&](Frag32<EX, EXACT> &f, int m, const Part &p) __attribute__((always_inline)) {
         read_rows(f, OX{}, p.rows + xlane + m * 32 * OX::kRow, xkey, p.scales + xslane + m * 512, p.kk);
     };
+    auto word_w = [&](int n, const Part &p) __attribute__((always_inline)) { return *(const unsigned *)(lds + p.scales + wslane + n * 512); };
+    auto word_x = [&](int m, const Part &p) __attribute__((always_inline)) { return *(const unsigned *)(lds + p.scales + xslane + m * 512); };
     // which bytes of this lane's scales count in a part (taken where they are used, not where they are read: no wait there).  Steps with
     // all their blocks go without: issue of instructions is what bounds the smaller tiles (512 x 4096 x 10240 on 4 bits 25.2 -> 22.8 us).
     struct Counts {
@@ -209,7 +211,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
         if constexpr (decltype(full)::value) return std::true_type{};
         else {
             const int block = (step * KK + kk) * 2;
-            return Counts{block + (EXACT ? 0 : h) < prm.nb ? 255u : 0u, block + 1 < prm.nb ? 255u : 0u};
+            return Counts{block + (EXACT ? 0 : h) < prm.nb ? ~0u : 0u, block + 1 < prm.nb ? ~0u : 0u};
         }
     };
     auto counted = [](unsigned scale, const auto &c, unsigned Counts::*which) __attribute__((always_inline)) {
@@ -217,7 +219,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
         else return scale;
     };
     v16f acc[TN][TM] = {};
-    auto multiply = [&](const Frag32<EW, EXACT> (&w)[TN], const Frag32<EX, EXACT> &x, int m, const auto &c) __attribute__((always_inline)) {
+    auto multiply = [&](auto part, const Frag32<EW, EXACT> (&w)[TN], const unsigned (&ws)[TN], const Frag32<EX, EXACT> &x, unsigned xs, int m, const auto &c) __attribute__((always_inline)) {
         if constexpr (EXACT) {
             auto bf16 = [&](const auto &g, bool wide, int i) __attribute__((always_inline)) {
                 const float s = __uint_as_float((i < 2 ? counted(g.scale, c, &Counts::b0) : counted(g.scale1, c, &Counts::b1)) << 23);
@@ -231,14 +233,14 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
                 for (int n = 0; n < TN; n++) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16(w[n], EW == kMx8, i), xb, acc[n][m], 0, 0, 0);
             }
         } else {
-            constexpr int FW = EW == kMx8 ? 0 : 4, FX = EX == kMx8 ? 0 : 4;
+            constexpr int FW = EW == kMx8 ? 0 : 4, FX = EX == kMx8 ? 0 : 4, kByte = decltype(part)::value % 2 * 2;
             auto codes = [](const v4i &lo, const v4i &hi, bool wide) __attribute__((always_inline)) {
                 return wide ? v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]} : v8i{lo[0], lo[1], lo[2], lo[3], 0, 0, 0, 0};
             };
 #pragma unroll
             for (int n = 0; n < TN; n++)
-                acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n].lo, w[n].hi, EW == kMx8), codes(x.lo, x.hi, EX == kMx8), acc[n][m], FW, FX, 0,
-                                                                            (int)counted(w[n].scale, c, &Counts::b0), 0, (int)counted(x.scale, c, &Counts::b0));
+                acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n].lo, w[n].hi, EW == kMx8), codes(x.lo, x.hi, EX == kMx8), acc[n][m], FW, FX, kByte,
+                                                                            (int)counted(ws[n], c, &Counts::b0), kByte, (int)counted(xs, c, &Counts::b0));
         }
     };
     // completes this wavefront's LDS reads, waits for no vector-memory operation
@@ -259,6 +261,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
         struct Set {
             Frag32<EW, EXACT> w[KK][TN];
             Frag32<EX, EXACT> x[KK][TM];
+            unsigned ws[KK / 2][TN], xs[KK / 2][TM];
         };
         Set sets[2];
         auto read_part = [&](Set &f, auto part, auto group, int step, int stage) __attribute__((always_inline)) {
@@ -266,9 +269,13 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
             const Part p = part_of(step, stage, kk);
             if constexpr (m == 0) {
 #pragma unroll
-                for (int n = 0; n < TN; n++) read_w(f.w[kk][n], n, p);
+                for (int n = 0; n < TN; n++) {
+                    read_w(f.w[kk][n], n, p);
+                    if constexpr (!EXACT && kk % 2 == 0) f.ws[kk / 2][n] = word_w(n, p);
+                }
             }
             read_x(f.x[kk][m], m, p);
+            if constexpr (!EXACT && kk % 2 == 0) f.xs[kk / 2][m] = word_x(m, p);
         };
         auto do_step = [&](auto whole, Set &now, Set &then, int i, int stage, int next) __attribute__((always_inline)) {
             wait_loads<(NST - 2) * LPS>();
@@ -277,7 +284,14 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
                 const auto c = counts_of(whole, i, decltype(part)::value);
                 static_for<TM>([&](auto group) __attribute__((always_inline)) {
                     constexpr int kk = decltype(part)::value, m = decltype(group)::value, slot = kk * TM + m;
-                    multiply(now.w[kk], now.x[kk][m], m, c);
+                    if constexpr (!EXACT && kk % 2 == 0) {
+                        if constexpr (m == 0) {
+#pragma unroll
+                            for (int n = 0; n < TN; n++) now.ws[kk / 2][n] >>= 8 * h;
+                        }
+                        now.xs[kk / 2][m] >>= 8 * h;
+                    }
+                    multiply(part, now.w[kk], now.ws[kk / 2], now.x[kk][m], now.xs[kk / 2][m], m, c);
                     __builtin_amdgcn_sched_barrier(0);
                     read_part(then, part, group, i + 1, next);
                     issue(i + NST, stage, std::integral_constant<int, slot * LPS / (KK * TM)>{}, std::integral_constant<int, (slot + 1) * LPS / (KK * TM)>{});
@@ -300,12 +314,19 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     } else {
         Frag32<EW, EXACT> fw[2][TN];                                   // this part's and the next one's
         Frag32<EX, EXACT> fx[TM];                                      // each read again as soon as it is multiplied
+        unsigned ws[TN], xs[TM], next_ws[TN], next_xs[TM];             // two parts' scales, and the next two's as they are read
         {
             const Part p = part_of(0, 0, 0);
 #pragma unroll
-            for (int n = 0; n < TN; n++) read_w(fw[0][n], n, p);
+            for (int n = 0; n < TN; n++) {
+                read_w(fw[0][n], n, p);
+                if constexpr (!EXACT) next_ws[n] = word_w(n, p);
+            }
 #pragma unroll
-            for (int m = 0; m < TM; m++) read_x(fx[m], m, p);
+            for (int m = 0; m < TM; m++) {
+                read_x(fx[m], m, p);
+                if constexpr (!EXACT) next_xs[m] = word_x(m, p);
+            }
         }
         // A step's KK parts.  A token group's operands are read again for the next part as soon as they are multiplied, the features'
         // into the other of two sets.  Behind the first products of a step's last part every read of this step has been made: the
@@ -320,7 +341,14 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
                 const auto c = counts_of(whole, i, kk);
                 static_for<TM>([&](auto group) __attribute__((always_inline)) {
                     constexpr int m = decltype(group)::value;
-                    multiply(fw[kk & 1], fx[m], m, c);
+                    if constexpr (!EXACT && kk % 2 == 0) {
+                        if constexpr (m == 0) {
+#pragma unroll
+                            for (int n = 0; n < TN; n++) ws[n] = next_ws[n] >> 8 * h;
+                        }
+                        xs[m] = next_xs[m] >> 8 * h;
+                    }
+                    multiply(part, fw[kk & 1], ws, fx[m], xs[m], m, c);
                     __builtin_amdgcn_sched_barrier(0);
                     if constexpr (m == 0) {
                         if constexpr (kk == KK - 1) {
@@ -328,9 +356,13 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
                             ring_barrier();
                         }
 #pragma unroll
-                        for (int n = 0; n < TN; n++) read_w(fw[~kk & 1][n], n, p);
+                        for (int n = 0; n < TN; n++) {
+                            read_w(fw[~kk & 1][n], n, p);
+                            if constexpr (!EXACT && kk % 2 == 1) next_ws[n] = word_w(n, p);
+                        }
                     }
                     read_x(fx[m], m, p);
+                    if constexpr (!EXACT && kk % 2 == 1) next_xs[m] = word_x(m, p);
                     constexpr int late = TM == 1 ? m : m - 1;
                     if constexpr (kk == KK - 1 && late >= 0 && late < kLate) issue_slot(i + NST, stage, std::integral_constant<int, late < 0 ? 0 : late>{});
                     if constexpr (kk == 0 && kSlots > kLate) issue_slot(i + NST - 1, last, std::integral_constant<int, kLate + m>{});
