@@ -203,7 +203,8 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     auto word_w = [&](int n, const Part &p) __attribute__((always_inline)) { return *(const unsigned *)(lds + p.scales + wslane + n * 512); };
     auto word_x = [&](int m, const Part &p) __attribute__((always_inline)) { return *(const unsigned *)(lds + p.scales + xslane + m * 512); };
     // which bytes of this lane's scales count in a part (taken where they are used, not where they are read: no wait there).  Steps with
-    // all their blocks go without: issue of instructions is what bounds the smaller tiles (512 x 4096 x 10240 on 4 bits 25.2 -> 22.8 us).
+    // all their blocks go without: the issue of instructions is what bounds the smaller tiles (512 x 4096 x 10240 on 4 bits, tiles of
+    // 64 x 128: 25.2 us with masks in every step, 22.8 without, 22.1 with the scales as words).
     struct Counts {
         unsigned b0, b1;
     };
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     if constexpr (WHOLE) {
         // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets, a few reads and
         // loads behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step:
-        // 256 x 4096 x 4096 on 8 by 4 bits 14.1 for 12.9 us).
+        // 256 x 4096 x 4096 on 8 by 4 bits a tenth more time).
         struct Set {
             Frag32<EW, EXACT> w[KK][TN];
             Frag32<EX, EXACT> x[KK][TM];
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     constexpr int kOctets = F / 8, kTokens = 64 / kOctets;             // octets of a token, tokens at a time
     const OctetEnd end(a, (n0 + wn0) / 8 + lane % kOctets);
     const bool inside = mrows == BM && n0 + BN <= a.N && (!a.q.codes || n0 + BN < a.N || a.N % 128 == 0);
-    // the largest tiles' results go past the cache where their rows are whole cache lines (8192 x 8192 x 8192: 280 -> 266 us)
+    // the largest tiles' results go past the cache where their rows are whole cache lines (8192 x 8192 x 8192 on 4 bits: 14 of 270 us)
     const bool past = BM == 256 && (a.q.codes ? ((uintptr_t)a.q.codes | a.q.ldc) % 128 == 0 : ((uintptr_t)a.y | a.ldy * 2) % 128 == 0);
     with_kind(a, [&](auto kind) __attribute__((always_inline)) {
         static_for<TM>([&](auto group) __attribute__((always_inline)) {
