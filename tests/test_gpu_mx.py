@@ -556,3 +556,61 @@ def test_rms_norm_of_rows_whose_squares_leave_the_range(B, dtype, K):
         same = B.quantize_mx(y.float())
         if dtype == "f32":
             assert torch.equal(q.codes, same.codes) and torch.equal(q.scales, same.scales)
+
+
+def test_tensors_of_more_than_four_gigabytes(B):
+    """Rows behind 2^32 bytes and 2^32 values of a tensor are converted, converted back and multiplied like the same rows alone."""
+    rows, K = (1 << 22) + 3, 1100
+    x = torch.empty(rows, K, device=DEV, dtype=torch.bfloat16)
+    x.view(-1)[:] = 0.5
+    some = torch.randn(70, K, device=DEV).bfloat16()
+    x[-70:] = some
+    q, alone = B.quantize_mx(x, B.MX8), B.quantize_mx(some, B.MX8)
+    assert torch.equal(q.codes[-70:], alone.codes) and torch.equal(q.scales[-70:], alone.scales)
+    assert torch.equal(q.codes[:70], q.codes[rows // 2:rows // 2 + 70])
+    assert torch.equal(B.dequantize_mx(q, torch.bfloat16, out=x)[-70:], B.dequantize_mx(alone, torch.bfloat16))
+    few = B.quantize_mx(torch.randn(3, K, device=DEV), B.MX4)
+    weights = lambda t, n: B.MxTensor(t.codes[:n], t.scales[:n], t.elem, t.k)
+    last = B.MxTensor(q.codes[-(1 << 22):], q.scales[-(1 << 22):], q.elem, q.k)             # as weights: 2^22 features
+    for variant in (2, 5, 6, 10):
+        y = B.linear_mx(few, last, variant=variant)
+        assert torch.equal(y[:, -70:], B.linear_mx(few, alone, variant=variant)), variant
+        assert torch.equal(y[:, :32], B.linear_mx(few, weights(last, 32), variant=variant)), variant
+
+
+def test_one_tensor_as_both_operands_and_rows_of_a_padded_batch(B):
+    """x times itself; rows that hold no numbers leave the others as they are."""
+    x = torch.randn(300, 260, device=DEV)
+    for elem in (B.MX4, B.MX8):
+        q = B.quantize_mx(x, elem)
+        copy = q._replace(codes=q.codes.clone(), scales=q.scales.clone())
+        want = B.linear_mx(q, copy, dtype=torch.float32)
+        assert torch.equal(B.linear_mx(q, q, dtype=torch.float32), want)
+        padded = copy._replace(codes=copy.codes.clone(), scales=copy.scales.clone())
+        padded.codes[100:150], padded.scales[100:150] = 0xff, 0xff
+        for variant in range(1, 11):
+            y, z = (B.linear_mx(t, q, dtype=torch.float32, variant=variant) for t in (copy, padded))
+            assert torch.equal(z[:100], y[:100]) and torch.equal(z[150:], y[150:]) and torch.isnan(z[100:150]).all(), variant
+
+
+def test_calls_from_two_threads(B):
+    import threading
+    x, w = B.quantize_mx(torch.randn(40, 500, device=DEV)), B.quantize_mx(torch.randn(130, 500, device=DEV), B.MX4)
+    h = torch.randn(40, 500, device=DEV, dtype=torch.bfloat16)
+    want = [B.linear_mx(x, w), B.linear_mx_q(x, w).codes, B.rms_norm_mx(h)[0].codes, B.quantize_mx(h).codes]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(stream):
+        with torch.cuda.stream(stream):
+            for _ in range(50):
+                got = [B.linear_mx(x, w), B.linear_mx_q(x, w).codes, B.rms_norm_mx(h)[0].codes, B.quantize_mx(h).codes]
+                stream.synchronize()
+                wrong.extend(i for i, (a, b) in enumerate(zip(got, want)) if not torch.equal(a, b))
+
+    threads = [threading.Thread(target=work, args=(torch.cuda.Stream(),)) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
