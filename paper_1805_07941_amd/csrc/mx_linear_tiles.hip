@@ -203,8 +203,8 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     auto word_w = [&](int n, const Part &p) __attribute__((always_inline)) { return *(const unsigned *)(lds + p.scales + wslane + n * 512); };
     auto word_x = [&](int m, const Part &p) __attribute__((always_inline)) { return *(const unsigned *)(lds + p.scales + xslane + m * 512); };
     // which bytes of this lane's scales count in a part (taken where they are used, not where they are read: no wait there).  Steps with
-    // all their blocks go without: the issue of instructions is what bounds the smaller tiles (512 x 4096 x 10240 on 4 bits, tiles of
-    // 64 x 128: 25.2 us with masks in every step, 22.8 without, 22.1 with the scales as words).
+    // all their blocks go without, their instructions are many beside the few products of a small tile's step (512 x 4096 x 10240 on
+    // 4 bits, tiles of 64 x 128: 25.2 us with masks in every step, 22.8 without, 22.1 with the scales as words).
     struct Counts {
         unsigned b0, b1;
     };
