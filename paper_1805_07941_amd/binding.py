@@ -24,6 +24,7 @@ MX_COVER, MX_FLOOR = 0, 1     # dfq_mx_rule
 LINEAR_AUTO, LINEAR_DIRECT = 0, 1      # dfq_linear_variant: these, and kernels by the tokens x features of a workgroup
 LINEAR_VARIANT_NAMES = {LINEAR_AUTO: "auto", LINEAR_DIRECT: "direct", 2: "stream 16x16", 3: "stream 16x32", 4: "stream 32x32", 5: "stream 32x64",
                         6: "tile 64x64", 7: "tile 64x128", 8: "tile 128x128", 9: "tile 128x128 deep", 10: "tile 256x256"}
+LINEAR_ALIGNED = 16           # added to any of them: products with an 8-bit operand aligned by eights, faster and less accurate (include/dfq.h)
 MX_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # dfq_dtype
 CAL_AMAX_WORDS = 256          # DFQ_CAL_AMAX_WORDS
 CALL_ARGS = 30                # DFQ_CALL_ARGS
@@ -496,7 +497,8 @@ def _linear_operands(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor]):
 
 def linear_mx(x: MxTensor, w: MxTensor, bias: Optional[torch.Tensor] = None, relu: bool = False, dtype: torch.dtype = torch.bfloat16,
               out: Optional[torch.Tensor] = None, stream=None, variant: int = LINEAR_AUTO) -> torch.Tensor:
-    """x [m, k] times w [n, k] transposed, plus bias [n] float32, with relu max(., 0): [m, n] of dtype."""
+    """x [m, k] times w [n, k] transposed, plus bias [n] float32, with relu max(., 0): [m, n] of dtype.  Products and sums are float32's;
+    variant=LINEAR_ALIGNED takes those with an 8-bit operand at up to twice the rate, 1.5e-5 off in the mean."""
     m, n, operands = _linear_operands(x, w, bias)
     code = _dtype_code(dtype)
     if out is None:

@@ -1145,9 +1145,10 @@ dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, s
                                  const float *bias, void *y, size_t ldy, dfq_dtype dtype, uint8_t *codes, size_t ldc, uint8_t *scales,
                                  size_t lds, dfq_mx_elem elem, dfq_mx_rule rule, size_t M, int N, int K, int relu, dfq_stream stream)
 {
+    const int aligned = variant >= DFQ_LINEAR_ALIGNED ? DFQ_LINEAR_ALIGNED : 0, kernel = variant - aligned;
     const LinearMxArgs a{x, x_scales, w, w_scales, ldx, ldxs, ldw, ldws, elem_x, elem_w, bias, y, ldy, dtype,
-                         MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, M, N, K, relu ? 1 : 0};
-    if (variant < DFQ_LINEAR_AUTO || variant > DFQ_LINEAR_TILE_256X256 || !dtype_ok(dtype) || !elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
+                         MxTensor{codes, ldc, scales, lds, elem}, rule == DFQ_MX_COVER, M, N, K, relu ? 1 : 0, aligned};
+    if (kernel < DFQ_LINEAR_AUTO || kernel > DFQ_LINEAR_TILE_256X256 || !dtype_ok(dtype) || !elem_ok(elem) || !rule_ok(rule)) return DFQ_EINVAL;
     if (N < 1 || K < 1) return DFQ_ESHAPE;
     if (!M) return DFQ_OK;
     if (!elem_ok(elem_x) || !elem_ok(elem_w) || (y && codes)) return DFQ_EINVAL;
@@ -1165,7 +1166,7 @@ dfq_status dfq_linear_mx_variant(dfq_linear_variant variant, const uint8_t *x, s
                 {bias, (size_t)N * 4}},
                {float_span(y, ldy, dtype, M, N), codes_span(codes, ldc, elem, M, N), codes ? scales_span(scales, lds, M, N) : Span{nullptr, 0}}))
         return DFQ_EINVAL;
-    const LinearMxForm form = (LinearMxForm)(int)variant;
+    const LinearMxForm form = (LinearMxForm)kernel;
     if (form != LinearMxForm::Auto && !linear_mx_supports(a, form)) return DFQ_EUNSUPPORTED;
     return from_hip(launch_linear_mx(a, form, (hipStream_t)stream));
 }
@@ -1269,7 +1270,7 @@ const CallEntry kCalls[] = {
     DFQ_ENTRY(dfq_eltwise_q), DFQ_ENTRY(dfq_concat_q_into), DFQ_ENTRY(dfq_pool_q), DFQ_ENTRY(dfq_quantize_np), DFQ_ENTRY(dfq_dequantize_np),
     DFQ_ENTRY(dfq_np_digits), DFQ_ENTRY(dfq_conv_np), DFQ_ENTRY(dfq_conv_np_add), DFQ_ENTRY(dfq_eltwise_np), DFQ_ENTRY(dfq_pool_np),
     DFQ_ENTRY(dfq_stem_pack_x), DFQ_ENTRY(dfq_quantize_mx), DFQ_ENTRY(dfq_dequantize_mx), DFQ_ENTRY(dfq_linear_mx), DFQ_ENTRY(dfq_linear_mx_q),
-    DFQ_ENTRY(dfq_rms_norm_mx)};
+    DFQ_ENTRY(dfq_linear_mx_variant),    DFQ_ENTRY(dfq_rms_norm_mx)};
 #undef DFQ_ENTRY
 constexpr int kNumCalls = (int)(sizeof(kCalls) / sizeof(kCalls[0]));
 

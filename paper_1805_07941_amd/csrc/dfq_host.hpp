@@ -145,6 +145,10 @@ struct LinearMxArgs {
     int cover;
     size_t M;
     int N, K, relu;
+    int aligned;            // DFQ_LINEAR_ALIGNED
+
+    // products with an 8-bit operand by the bfloat16 instructions (mx_linear.hpp)
+    bool exact() const { return (elem_x || elem_w) && !aligned; }
 };
 
 hipError_t launch_quantize_mx(const MxRows &x, const MxTensor &q, bool cover, hipStream_t st);

@@ -7,7 +7,7 @@ namespace {
 
 // Microseconds of a call: fixed + rounds * (tile + depth * K / 1000) + load * K / 1e6 * (byte * bytes + product * products), with K in
 // whole 256s, rounds the workgroups that a compute unit gets at most and load the same, bytes what a workgroup reads of its operands
-// for one k and products its tile's, twice for an 8-bit operand and four times for the bfloat16 form that float32 results of one need.
+// for one k and products its tile's, twice for an aligned 8-bit operand and four times for the bfloat16 form.
 // `shared`: two workgroups of a compute unit overlap, so that load is nearer to what the units get in the mean.  Fitted to 1892 calls
 // (1 to 8192 tokens, 32 to 16384 features, K 64 to 16384, every pair of elements) under every form that could be near: each form's
 // times within 7 to 14 % of its line in the mean, and the form the lines choose 1.024 times the fastest one's time in the mean (calls
@@ -40,8 +40,8 @@ double form_time(const FormTime &f, const LinearMxArgs &a)
         if (load < 1) load = 1;
     }
     const int bx = a.elem_x ? 8 : 4, bw = a.elem_w ? 8 : 4;
-    const bool wide = bx == 8 || bw == 8, exact = wide && !a.q.codes && a.dtype == 0;
-    const double bytes = (f.tokens * bx + f.features * bw) / 8.0, products = (double)f.tokens * f.features * (exact ? 4 : wide ? 2 : 1);
+    const bool wide = bx == 8 || bw == 8;
+    const double bytes = (f.tokens * bx + f.features * bw) / 8.0, products = (double)f.tokens * f.features * (a.exact() ? 4 : wide ? 2 : 1);
     const double K = (a.K + 255) / 256 * 256;
     return f.fixed + rounds * (f.tile + f.depth * K * 1e-3) + load * K * 1e-6 * (f.byte * bytes + f.product * products);
 }

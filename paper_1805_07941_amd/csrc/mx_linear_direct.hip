@@ -14,7 +14,7 @@ namespace dfq {
 namespace {
 
 // EXACT: the elements times their scales as bfloat16 (they fit its significand) on the bfloat16 matrix instructions, whose products
-// and sums keep float32's accuracy; see launch_linear_mx.
+// and sums keep float32's accuracy (mx_linear.hpp).
 template <int EX, int EW, bool EXACT, int FT, int TT, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) linear_mx_direct_kernel(LinearMxArgs a)
 {
@@ -118,10 +118,10 @@ hipError_t run(const LinearMxArgs &a, hipStream_t st)
 }
 
 template <int EX, int EW>
-hipError_t by_output(const LinearMxArgs &a, hipStream_t st)
+hipError_t by_accuracy(const LinearMxArgs &a, hipStream_t st)
 {
     if constexpr (EX == kMx8 || EW == kMx8)
-        if (!a.q.codes && a.dtype == kF32) return run<EX, EW, true, 2, 1, 4, 2>(a, st);
+        if (a.exact()) return run<EX, EW, true, 2, 1, 4, 2>(a, st);
     return run<EX, EW, false, 2, 1, 4, 2>(a, st);
 }
 
@@ -129,8 +129,8 @@ hipError_t by_output(const LinearMxArgs &a, hipStream_t st)
 
 hipError_t launch_linear_mx_direct(const LinearMxArgs &a, hipStream_t st)
 {
-    if (a.elem_x == kMx4) return a.elem_w == kMx4 ? by_output<kMx4, kMx4>(a, st) : by_output<kMx4, kMx8>(a, st);
-    return a.elem_w == kMx4 ? by_output<kMx8, kMx4>(a, st) : by_output<kMx8, kMx8>(a, st);
+    if (a.elem_x == kMx4) return a.elem_w == kMx4 ? by_accuracy<kMx4, kMx4>(a, st) : by_accuracy<kMx4, kMx8>(a, st);
+    return a.elem_w == kMx4 ? by_accuracy<kMx8, kMx4>(a, st) : by_accuracy<kMx8, kMx8>(a, st);
 }
 
 }  // namespace dfq

@@ -176,7 +176,7 @@ hipError_t by_shape(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 
 hipError_t launch_linear_mx_stream(const LinearMxArgs &a, LinearMxForm form, hipStream_t st)
 {
-    const bool exact = !a.q.codes && a.dtype == kF32;
+    const bool exact = a.exact();
     if (a.elem_x == kMx4 && a.elem_w == kMx4) return by_shape<kMx4, kMx4, false>(a, form, st);
     if (a.elem_x == kMx4) return exact ? by_shape<kMx4, kMx8, true>(a, form, st) : by_shape<kMx4, kMx8, false>(a, form, st);
     if (a.elem_w == kMx4) return exact ? by_shape<kMx8, kMx4, true>(a, form, st) : by_shape<kMx8, kMx4, false>(a, form, st);
