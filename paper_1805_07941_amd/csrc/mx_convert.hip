@@ -188,12 +188,15 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
         mean = squares(c, std::true_type{}) / (float)K + p.a.eps * c * c;
     }
     const float r = 1.0f / sqrtf(mean);
+    // A value times c times r: the factor above 1 before r and the one below 1 behind it, so that nothing between leaves float32's range
+    // (a row with 2^51 has c = 2^-76, and its values below 2^-50 must not be multiplied by that first).
+    const float before = fmaxf(c, 1.0f), behind = fminf(c, 1.0f);
 
     auto finish = [&](float (&v)[8], float (&g)[8], int o) __attribute__((always_inline)) {
         if (!EARLY) load_weight<DT>(g, p, o);
         if (p.a.sum) store_octet<DT, true>(v, (char *)p.a.sum + row * p.a.ldsum * B, o, K);
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * c * r * g[i] : 0.0f;      // (zeros behind K whatever r is)
+        for (int i = 0; i < 8; i++) v[i] = o * 8 + i < K ? v[i] * before * r * behind * g[i] : 0.0f;      // (zeros behind K whatever r is)
         if (p.a.y) store_octet<DT, true>(v, (char *)p.a.y + row * p.a.ldy * B, o, K);
         if (p.a.q.codes) mx_store_octet<ELEM>(v, p.a.q.codes + row * p.a.q.ldc, p.a.q.scales + row * p.a.q.lds, o, p.nb, p.a.cover);
     };
