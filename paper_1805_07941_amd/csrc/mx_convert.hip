@@ -97,7 +97,7 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 // R threads to a row (a wavefront's part, a wavefront or a workgroup), V octets of the sum held in registers between the two passes
 // over it; V == 0: rows too long for that, the second pass reads x and add again.  Bound by the bytes: x and add read, the sum and the
 // codes written (8192 x 8192 bfloat16 to 8 bits, 473 MB: 93 us, 5.1 TB/s; a copy of that size 5.1 to 5.3).
-// The sum of squares is a float32 one (in 64 bits that call took 104 us).  Squares that leave float32's range (values of 2^50 and
+// The sum of squares is a float32 one (in 64 bits that call took 104 us), but for a thread's part of the longest rows.  Squares that leave float32's range (values of 2^50 and
 // above, 2^-40 and below) are added again, of values times a power of two.
 // The sum goes past the cache; the codes stay, the product behind the norm reads them: 8192 x 8192 codes past it 78 us, but norm and
 // product 518 for 509, 16384 x 4096 with its product 314 for 295.
@@ -165,10 +165,16 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
                     if (j * R + first < octets) load_weight<DT>(w[j], p, j * R + first);
             }
         } else {
+            // up to 512 octets to a thread: each is added up on its own and they meet in 64 bits, where thousands of additions that round
+            // the same way gather nothing (2^22 equal values by float32 alone: 260 of its steps off)
+            double wide = 0.0;
             for (int o = first; o < octets; o += R) {
                 load_sum<DT>(s[0], p, row, o);
+                sq = 0.0f;
                 visit(s[0]);
+                wide += (double)sq;
             }
+            sq = (float)wide;
         }
 #pragma unroll
         for (int off = (R < 64 ? R : 64) / 2; off >= 1; off >>= 1) sq += __shfl_xor(sq, off, kWave);

@@ -30,3 +30,17 @@ def test_small_values_beside_large_ones(B, dtype, K):
         if dtype == "f32":
             same = B.quantize_mx(y)
             assert torch.equal(q.codes, same.codes) and torch.equal(q.scales, same.scales)
+
+
+@pytest.mark.parametrize("value", [1.05, 1.1, 1.3, 3.3])
+@pytest.mark.parametrize("K", [40000, 1 << 20, (1 << 22) - 5])
+def test_long_rows_of_one_value(B, K, value):
+    """Every addition of equal squares rounds the same way: a sum of thousands by one thread must not gather that."""
+    x = torch.full((2, K), value, device=DEV)
+    x[1] = -value
+    for eps in (0.0, 1e-3):
+        _, y, _ = B.rms_norm_mx(x, None, eps, elem=None, want_y=True)
+        d = float(np.float32(value))
+        v = d / np.sqrt(d * d + float(np.float32(eps)))
+        off = np.abs(np.abs(host(y)) - v).max() / v
+        assert off <= NORM_U, off / NORM_U * 64
