@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
             }
         } else {
             // up to 512 octets to a thread: each is added up on its own and they meet in 64 bits, where thousands of additions that round
-            // the same way gather nothing (2^22 equal values by float32 alone: 260 of its steps off)
+            // the same way gather nothing (2^22 equal values: 2 steps of float32 off, 260 without)
             double wide = 0.0;
             for (int o = first; o < octets; o += R) {
                 load_sum<DT>(s[0], p, row, o);
@@ -188,12 +188,14 @@ __global__ void __launch_bounds__(T) rms_norm_mx_kernel(NormParams p)
         }
         return sq;
     };
-    float c = 1.0f, sq = squares(1.0f, std::false_type{}), mean = sq / (float)K + p.a.eps;
+    float c = 1.0f, lift = 1.0f, sq = squares(1.0f, std::false_type{}), mean = sq / (float)K + p.a.eps;
     if (!(sq <= 0x1p100f) || mean < 0x1p-80f) {          // (the same for all of a row's threads)
-        c = sq <= 0x1p100f ? 0x1p90f : 0x1p-76f;       // (2^22 squares of up to 2^128 or down to 2^-149 stay normal)
-        mean = squares(c, std::true_type{}) / (float)K + p.a.eps * c * c;
+        // 2^22 squares of values up to 2^128 or a single one of 2^-149 stay normal; the mean of such a one among zeros does times 2^24
+        c = sq <= 0x1p100f ? 0x1p90f : 0x1p-76f;
+        lift = c > 1.0f ? 0x1p24f : 1.0f;
+        mean = squares(c, std::true_type{}) * (lift / (float)K) + p.a.eps * c * c * lift;
     }
-    const float r = 1.0f / sqrtf(mean);
+    const float r = (lift > 1.0f ? 0x1p12f : 1.0f) / sqrtf(mean);
     // A value times c times r: the factor above 1 before r and the one below 1 behind it, so that nothing between leaves float32's range
     // (a row with 2^51 has c = 2^-76, and its values below 2^-50 must not be multiplied by that first).
     const float before = fmaxf(c, 1.0f), behind = fminf(c, 1.0f);

@@ -44,3 +44,16 @@ def test_long_rows_of_one_value(B, K, value):
         v = d / np.sqrt(d * d + float(np.float32(eps)))
         off = np.abs(np.abs(host(y)) - v).max() / v
         assert off <= NORM_U, off / NORM_U * 64
+
+
+@pytest.mark.parametrize("K", [1 << 15, 3 << 20, (1 << 22) - 5])
+def test_a_smallest_value_among_zeros(B, K):
+    """One value of 1 to 5 times 2^-149 in a long row: the mean square is far below float32's smallest numbers, its root is not."""
+    x = torch.zeros(3, K, device=DEV)
+    for r, n in enumerate((1, 3, 5)):
+        x[r, 7 * r] = float(n * 2.0 ** -149)
+    _, y, _ = B.rms_norm_mx(x, None, 0.0, elem=None, want_y=True)
+    y = host(y)
+    for r in range(3):
+        assert abs(y[r, 7 * r] / np.sqrt(K) - 1) <= NORM_U, (r, abs(y[r, 7 * r] / np.sqrt(K) - 1) / NORM_U * 64)
+    assert np.count_nonzero(y) == 3
