@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kBlock) dequantize_mx_kernel(const uint8_t *__
         float *p = (float *)to + o * 4;
         const int left = K - o * 4;
         if (left >= 4) {
-            store_as<true>((f32x4_any *)p, f32x4{v[0], v[1], v[2], v[3]});
+            store_any<true>((f32x4_any *)p, f32x4{v[0], v[1], v[2], v[3]});
         } else {
 #pragma unroll
             for (int i = 0; i < 4; i++)

@@ -92,8 +92,21 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b)
 }
 
 // NT: results that are written once and too many for a cache to hold go past it
-template <bool NT, class P, class T>
-__device__ __forceinline__ void store_as(P *p, const T &v)
+template <bool NT, class T>
+__device__ __forceinline__ void store_as(T *p, const T &v)
+{
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+// 16 bytes at any address of their element type (no template of the pointer's: a template's argument loses the alignment)
+template <bool NT>
+__device__ __forceinline__ void store_any(u32x4_any *p, u32x4 v)
+{
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool NT>
+__device__ __forceinline__ void store_any(f32x4_any *p, f32x4 v)
 {
     if constexpr (NT) __builtin_nontemporal_store(v, p);
     else *p = v;
@@ -111,7 +124,7 @@ __device__ __forceinline__ void store_octet(const float (&v)[8], void *row, int 
             ((f32x4_any *)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
             ((f32x4_any *)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
         } else {
-            store_as<NT>((u32x4_any *)p, u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])});
+            store_any<NT>((u32x4_any *)p, u32x4{pack_pair<DT>(v[0], v[1]), pack_pair<DT>(v[2], v[3]), pack_pair<DT>(v[4], v[5]), pack_pair<DT>(v[6], v[7])});
         }
         return;
     }
