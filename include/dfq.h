@@ -141,7 +141,8 @@ dfq_status dfq_dequantize_mx(const uint8_t *codes, size_t ldc, const uint8_t *sc
 /* y[m][n] = sum_k x[m][k] * w[n][k] + bias[n] (bias: N floats or NULL), with relu max(., 0), rounded once to dtype.
  * x: M rows of K, w: N rows of K, both microscaled and each with its own elements; y: M rows of N, ldy elements apart.
  * Products and sums are float32's, whatever the result's type; DFQ_LINEAR_ALIGNED below is faster and
- * less accurate.  Sums below 2^-126 may become 0. */
+ * less accurate.  Sums below 2^-126 may become 0.  With an 8-bit operand an element times its scale is taken as a bfloat16: exact from scale
+ * byte 3 on, a multiple of 2^-133 below, infinite from 2^128 on; two 4-bit operands, and DFQ_LINEAR_ALIGNED, take every scale as it is. */
 dfq_status dfq_linear_mx(const uint8_t *x, size_t ldx, const uint8_t *x_scales, size_t ldxs, dfq_mx_elem elem_x, const uint8_t *w, size_t ldw,
                          const uint8_t *w_scales, size_t ldws, dfq_mx_elem elem_w, const float *bias, void *y, size_t ldy, dfq_dtype dtype,
                          size_t M, int N, int K, int relu, dfq_stream stream);

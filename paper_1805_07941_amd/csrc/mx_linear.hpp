@@ -30,7 +30,7 @@ __host__ inline void advance_tokens(LinearMxArgs &a, size_t m)
     }
 }
 
-// eight codes times their scale as bfloat16, which holds them exactly
+// eight codes times their scale as bfloat16, which holds their digits and, from scale byte 3 (E2M1: 0) on and below 2^128, their powers
 __device__ __forceinline__ v8bf bf16_of_mx8(int lo, int hi, float scale)
 {
     const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);

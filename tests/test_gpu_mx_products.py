@@ -113,3 +113,62 @@ def test_aligned_products_in_a_list_of_calls(B):
     args = (B.LINEAR_ALIGNED, *at(x), *at(w), b.data_ptr(), y.data_ptr(), 40, 1, None, 0, None, 0, 0, 0, 9, 40, 300, 0)
     B.CallList([(B.lib().dfq_linear_mx_variant, args)]).run(torch.cuda.current_stream().cuda_stream)
     assert torch.equal(y, want)
+
+
+def at_scales(rng, rows, K, elem, scale):
+    """Codes of every kind but NaN in blocks of one scale."""
+    codes = rng.integers(0, 256, (rows, K * elem // 8), dtype=np.uint8)
+    if elem == 8:
+        codes[(codes & 0x7f) == 0x7f] = 0x38
+    return codes, np.full((rows, -(-K // 128) * 4), scale, np.uint8)
+
+
+@pytest.mark.parametrize("sx, sw", [(0, 240), (1, 235), (3, 240), (8, 230), (240, 0), (240, 3), (246, 6), (230, 8), (4, 246)])
+@pytest.mark.parametrize("ex, ew", PAIRS)
+def test_scales_at_the_ends_of_their_range(B, ex, ew, sx, sw):
+    """One operand's blocks with the smallest scales, the other's with large ones, and the other way round: the sums are ordinary numbers.
+    As a bfloat16 an element of 8 bits times its scale is a multiple of 2^-133, half of which is what it may be off by below scale byte 3."""
+    M, N, K = 66, 70, 160
+    rng = rng_of("ends", ex, ew, sx, sw)
+    qx, qw = at_scales(rng, M, K, ex, sx), at_scales(rng, N, K, ew, sw)
+    vx, vw = mx.values(*qx, ELEM[ex], K), mx.values(*qw, ELEM[ew], K)
+    x, w = on_gpu(B, qx, ex, K), on_gpu(B, qw, ew, K)
+    want = mx.linear(vx, vw)
+    exact, aligned = (product_bound(vx, vw, None, (ex, ew), e) for e in (True, False))
+    if 8 in (ex, ew):
+        exact = exact + (2.0 ** -134 * np.abs(vw).sum(1) if ex == 8 and sx < 3 else 0) + (2.0 ** -134 * np.abs(vx).sum(1)[:, None] if ew == 8 and sw < 3 else 0)
+    for variant in VARIANTS:
+        for how, err in ((0, exact), (B.LINEAR_ALIGNED, aligned)):
+            for out in TYPES:
+                y = host(B.linear_mx(x, w, dtype=TYPES[out], variant=variant + how))
+                tol = err + HALF[out] * (np.abs(want) + err) + (2.0 ** -25 if out == "f16" else 0)
+                with np.errstate(invalid="ignore"):
+                    ok = (np.abs(y - want) <= tol) | ((out == "f16") & np.isinf(y) & (np.abs(want) + tol > 65504))
+                assert ok.all(), (variant, how, out, np.argwhere(~ok)[:4], np.nanmax(np.abs(y - want) / tol))
+
+
+@pytest.mark.parametrize("ex, ew", [(8, 4), (8, 8), (4, 8)])
+def test_elements_beyond_float32(B, ex, ew):
+    """2^128 and above, which no conversion of float32 values writes but for values next to it: infinite where elements are taken as
+    bfloat16, numbers where they are aligned.  Rows without such elements are what they are."""
+    M, N, K = 20, 40, 96
+    rng = rng_of("beyond", ex, ew)
+    flip = ex == 4                                       # the operand with the large scales is the 8-bit one
+    big, other = at_scales(rng, N if flip else M, K, 8, 250), at_scales(rng, M if flip else N, K, ew if not flip else ex, 10)
+    eo = ex if flip else ew
+    big[0][:] &= 0x87                                    # below 2^-5: subnormal elements
+    big[0][::2, 33] = 0x7e                               # 448 * 2^123
+    zero = (other[0] & 0x7f) == 0 if eo == 8 else True
+    other[0][...] = np.where(zero, other[0] | (1 if eo == 8 else 0x11), other[0])                  # nothing is multiplied by zero
+    values = mx.values(*big, mx.MX8, K), mx.values(*other, ELEM[eo], K)
+    vx, vw = (values[1], values[0]) if flip else values
+    b, o = on_gpu(B, big, 8, K), on_gpu(B, other, eo, K)
+    x, w = (o, b) if flip else (b, o)
+    want, beyond = mx.linear(vx, vw), np.zeros((M, N), bool)
+    beyond[(slice(None), slice(None, None, 2)) if flip else slice(None, None, 2)] = True
+    exact, aligned = (product_bound(vx, vw, None, (ex, ew), e) for e in (True, False))
+    for variant in VARIANTS:
+        y = host(B.linear_mx(x, w, dtype=torch.float32, variant=variant))
+        assert not np.isfinite(y[beyond]).any() and (np.abs(y - want) <= exact + U * np.abs(want))[~beyond].all(), variant
+        y = host(B.linear_mx(x, w, dtype=torch.float32, variant=variant + B.LINEAR_ALIGNED))
+        assert (np.abs(y - want) <= aligned + U * np.abs(want)).all(), variant
