@@ -1,5 +1,7 @@
 """Products on microscaled operands where they are hardest to hold: sums that cancel, blocks that hold no numbers, scales at the ends of their
 range, long reductions through the tile kernels.  Bounds as in test_gpu_mx.py: float32's step u = 2^-24 and half a step of the result's type."""
+import functools
+
 import numpy as np
 import pytest
 
@@ -25,6 +27,22 @@ def codes_of(v, elem):
     return (c[:, 0::2] | c[:, 1::2] << 4 if elem == 4 else c), scales
 
 
+def scale_bytes(amax, elem, rule):
+    """oracle/mx.py's scale_byte for an array of finite magnitudes."""
+    powers, top = np.exp2(np.arange(255.0) - 127), mx.magnitudes(ELEM[elem])[-1]
+    if rule == mx.COVER:
+        return np.searchsorted(top * powers, amax)
+    return np.maximum(np.searchsorted(2.0 ** np.floor(np.log2(top)) * powers, amax, side="right") - 1, 0)
+
+
+def test_scale_bytes_are_the_oracles():
+    rng = rng_of("bytes")
+    v = np.concatenate(([0.0, 6.0, 448.0, 4.0, 256.0, 8.0, 512.0, 2.0 ** -149], np.exp2(rng.uniform(-140, 120, 40))))
+    for elem in (4, 8):
+        for rule in (mx.COVER, mx.FLOOR):
+            assert scale_bytes(v, elem, rule).tolist() == [mx.scale_byte(a, ELEM[elem], rule) for a in v]
+
+
 def converted_within(B, q, want, err, elem, rule):
     """A converted result [M, N] against the sums it stands for, each known to within err."""
     M, N = want.shape
@@ -32,10 +50,8 @@ def converted_within(B, q, want, err, elem, rule):
     codes, scales = host(q.codes), host(q.scales)
     wide, ewide = (np.pad(v, ((0, 0), (0, nb * 32 - N))) for v in (want, err))
     amax, slack = np.abs(wide).reshape(M, nb, 32).max(2), ewide.reshape(M, nb, 32).max(2)
-    for m in range(M):
-        for k in range(nb):
-            lo, hi = (mx.scale_byte(max(a, 0.0), ELEM[elem], rule) for a in (amax[m, k] - slack[m, k], amax[m, k] + slack[m, k]))
-            assert lo <= scales[m, k] <= hi, (m, k, scales[m, k], lo, hi)
+    lo, hi = (scale_bytes(np.maximum(a, 0), elem, rule) for a in (amax - slack, amax + slack))
+    assert ((lo <= scales[:, :nb]) & (scales[:, :nb] <= hi)).all()
     assert not scales[:, nb:].any()
     got = mx.values(codes, scales, ELEM[elem], nb * 32)
     assert not got[:, N:].any()
@@ -84,13 +100,18 @@ def test_sums_that_cancel(B, ex, ew, M, N, K):
 ALIGNED_SHAPES = [(1, 1, 1), (3, 35, 97), (16, 32, 300), (33, 65, 513), (70, 100, 1025), (130, 140, 1600), (257, 300, 700)]
 
 
+@functools.lru_cache(maxsize=None)
+def aligned_case(B, ex, ew, M, N, K):
+    gpu, (vx, vw, vb) = products(B, rng_of("aligned", ex, ew, M, N, K), M, N, K, ex, ew, True)
+    return gpu, mx.linear(vx, vw, vb), product_bound(vx, vw, vb, (ex, ew), False)
+
+
 @pytest.mark.parametrize("variant", VARIANTS)
 @pytest.mark.parametrize("ex, ew", PAIRS)
 def test_aligned_products(B, ex, ew, variant):
     """What a caller asks for by LINEAR_ALIGNED: within what the alignment of eight products adds; on 4-bit operands nothing changes."""
     for M, N, K in ALIGNED_SHAPES:
-        (x, w, b), (vx, vw, vb) = products(B, rng_of("aligned", ex, ew, M, N, K), M, N, K, ex, ew, True)
-        want, err = mx.linear(vx, vw, vb), product_bound(vx, vw, vb, (ex, ew), False)
+        (x, w, b), want, err = aligned_case(B, ex, ew, M, N, K)
         for out in TYPES:
             got = B.linear_mx(x, w, b, dtype=TYPES[out], variant=variant + B.LINEAR_ALIGNED)
             tol = err + HALF[out] * (np.abs(want) + err) + (2.0 ** -25 if out == "f16" else 0)
@@ -172,3 +193,32 @@ def test_elements_beyond_float32(B, ex, ew):
         assert not np.isfinite(y[beyond]).any() and (np.abs(y - want) <= exact + U * np.abs(want))[~beyond].all(), variant
         y = host(B.linear_mx(x, w, dtype=torch.float32, variant=variant + B.LINEAR_ALIGNED))
         assert (np.abs(y - want) <= aligned + U * np.abs(want)).all(), variant
+
+
+@pytest.mark.parametrize("ex, ew", PAIRS)
+def test_blocks_that_hold_no_numbers(B, ex, ew):
+    """A NaN block as the converter writes it, scale byte 255 over zero codes: every sum that reads it is NaN, the others are what they
+    were, by every kernel and in every type; against values, zeros and another such block."""
+    M, N, K = 70, 72, 416
+    rng = rng_of("nan blocks", ex, ew)
+    vx, vw = rng.standard_normal((M, K)).astype(np.float32), rng.standard_normal((N, K)).astype(np.float32)
+    vx[3, 40], vx[66, 0], vx[67, K - 1] = np.nan, np.inf, -np.inf
+    vw[7, 200], vw[70, K - 1], vw[71, 0] = np.nan, -np.inf, np.inf
+    vx[20], vw[30] = 0, 0
+    x, w = B.quantize_mx(torch.from_numpy(vx).to(DEV), ELEM[ex]), B.quantize_mx(torch.from_numpy(vw).to(DEV), ELEM[ew])
+    assert (host(x.scales)[[3, 66, 67], [1, 0, 12]] == 255).all() and not host(x.codes)[3, ex * 4:ex * 8].any()
+    clean_x, clean_w = vx.copy(), vw.copy()
+    clean_x[[3, 66, 67]], clean_w[[7, 70, 71]] = 0, 0
+    cx, cw = B.quantize_mx(torch.from_numpy(clean_x).to(DEV), ELEM[ex]), B.quantize_mx(torch.from_numpy(clean_w).to(DEV), ELEM[ew])
+    bad = np.zeros((M, N), bool)
+    bad[[3, 66, 67]], bad[:, [7, 70, 71]] = True, True
+    spoilt = np.stack([bad[:, k:k + 32].any(1) for k in range(0, N, 32)], 1).repeat(32, 1)[:, :N]
+    for variant in (*VARIANTS, B.LINEAR_ALIGNED, *(v + B.LINEAR_ALIGNED for v in VARIANTS[1:])):
+        for out in TYPES:
+            for relu in (False, True):
+                y, clean = (host(B.linear_mx(a, b, None, relu, TYPES[out], variant=variant)) for a, b in ((x, w), (cx, cw)))
+                assert np.array_equal(np.isnan(y), bad), (variant, out, relu)
+                assert np.array_equal(y[~bad], clean[~bad]), (variant, out, relu)
+        if variant & 15 != HALF_A_BLOCK:
+            for elem in (4, 8):
+                assert np.array_equal(np.isnan(host(B.dequantize_mx(B.linear_mx_q(x, w, elem=ELEM[elem], relu=True, variant=variant)))), spoilt), (variant, elem)
