@@ -227,7 +227,7 @@ _ZEROS = [0] * CALL_ARGS
 class CallList:
     """[(C function, its arguments but the stream)] as one library call.  Holds what the arguments point to on the host.  input_ptr: the address
     of the pass's input among the arguments, which rebind() replaces (a record is 30 words and a pass 56 of them: 0.2 ms to build)."""
-    _numbers = {}
+    _numbers = {}                                             # name -> (its number, which of its arguments are floats)
 
     def __init__(self, calls, input_ptr: Optional[int] = None):
         words, arrays = [], {}                                # arrays of addresses by their own
@@ -240,14 +240,13 @@ class CallList:
 
         for fn, args in calls:
             name = fn.__name__
-            number = self._numbers.get(name)
-            if number is None:
-                number = self._numbers[name] = lib().dfq_call_number(name.encode())
+            known = self._numbers.get(name)
+            if known is None:
+                known = self._numbers[name] = (lib().dfq_call_number(name.encode()), [i for i, t in enumerate(fn.argtypes) if t is C.c_float])
+            number, floats = known
             words.append((number & 0xffffffff) | len(args) << 32)
-            if C.c_float in fn.argtypes:
-                args = [float(a) if t is C.c_float else a for a, t in zip(args, fn.argtypes)]
-            words += [a if type(a) is int else a.frac if type(a) is Fmt else 0 if a is None else of_array(a) if isinstance(a, C.Array) else
-                      struct.unpack("<I", struct.pack("<f", a))[0] if type(a) is float else int(a) for a in args]
+            words += [a if type(a) is int else a.frac if type(a) is Fmt else 0 if a is None else of_array(a) if isinstance(a, C.Array) else int(a)
+                      for a in (args if not floats else [struct.unpack("<I", bytes(C.c_float(a)))[0] if i in floats else a for i, a in enumerate(args)])]
             words += _ZEROS[len(args):]
         self._held, self._count = calls, len(calls)
         self._input, self._arrays, self._at = input_ptr, arrays, None
