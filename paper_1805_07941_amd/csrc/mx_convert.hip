@@ -96,9 +96,9 @@ hipError_t run_dequantize(const MxTensor &q, const MxRows &x, hipStream_t st)
 // ---- root-mean-square norm: s = x + add, y = s / sqrt(mean(s^2) + eps) * weight.
 // R threads to a row (a wavefront's part, a wavefront or a workgroup), V octets of the sum held in registers between the two passes
 // over it; V == 0: rows too long for that, the second pass reads x and add again.  Bound by the bytes: x and add read, the sum and the
-// codes written (8192 x 8192 bfloat16 to 8 bits, 473 MB: 93 us, 5.1 TB/s; a copy of that size 5.1 to 5.3).
-// The sum of squares is a float32 one (in 64 bits that call took 104 us), but for a thread's part of the longest rows.  Squares that leave float32's range (values of 2^50 and
-// above, 2^-40 and below) are added again, of values times a power of two.
+// codes written (8192 x 8192 bfloat16 to 8 bits, 472 MB: 88 us, 5.4 TB/s; a copy of that size 5.1 to 5.3).
+// The sum of squares is a float32 one (in 64 bits that call took a ninth longer), but for a thread's part of the longest rows.
+// Squares that leave float32's range (values of 2^50 and above, 2^-40 and below) are added again, of values times a power of two.
 // The sum goes past the cache; the codes stay, the product behind the norm reads them: 8192 x 8192 codes past it 78 us, but norm and
 // product 518 for 509, 16384 x 4096 with its product 314 for 295.
 struct NormParams {

@@ -113,7 +113,7 @@ __device__ __forceinline__ void store_any(f32x4_any *p, f32x4 v)
 }
 
 // the values of an octet rounded to the row's type and stored; nothing past K.  (float32: two stores that take turns in a cache line,
-// which do not go past the cache: 8192 x 8192 converted back 64 us, past it 104.)
+// which do not go past the cache: a conversion back of 8192 x 8192 by such stores took 64 us, past it 104.)
 template <int DT, bool NT = false>
 __device__ __forceinline__ void store_octet(const float (&v)[8], void *row, int o, int K)
 {

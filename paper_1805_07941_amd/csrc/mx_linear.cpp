@@ -9,9 +9,10 @@ namespace {
 // whole 256s, rounds the workgroups that a compute unit gets at most and load the same, bytes what a workgroup reads of its operands
 // for one k and products its tile's, twice for an aligned 8-bit operand and four times for the bfloat16 form.
 // `shared`: two workgroups of a compute unit overlap, so that load is nearer to what the units get in the mean.  Fitted to 1892 calls
-// (1 to 8192 tokens, 32 to 16384 features, K 64 to 16384, every pair of elements) under every form that could be near: each form's
-// times within 7 to 14 % of its line in the mean, and the form the lines choose 1.024 times the fastest one's time in the mean (calls
-// of 8 us and more: 1.016).
+// (1 to 8192 tokens, 32 to 16384 features, K 64 to 16384; 4 by 4, 8 by 4 and 8 by 8 bits, the last two aligned and not) under every
+// form that could be near: each form's times within 7 to 14 % of its line in the mean, and the form the lines choose 1.024 times the
+// fastest one's time in the mean (calls of 8 us and more: 1.016).  Other calls: 423 of 8 by 4, 8 by 8 and 4 by 8 bits 1.019, 141 of
+// 4 by 8 aligned 1.011.
 struct FormTime {
     LinearMxForm form;
     int tokens, features;

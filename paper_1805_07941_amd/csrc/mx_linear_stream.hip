@@ -1,8 +1,8 @@
 // The inner product on microscaled operands for few results: what bounds it is the bytes of the weights and a call's latency.
 //
 // A workgroup has FT * 16 features and TT * 16 tokens; its wavefronts share the reduction axis, each with chunks of 256 values of its
-// own, and their sums meet in LDS in a fixed order at the end.  A chunk comes by direct global -> LDS loads into a ring of two stages
-// that belongs to the wavefront alone: nothing but its own count of outstanding loads is waited for.  (Loads straight into the
+// own, and their sums meet in LDS in a fixed order at the end.  A chunk comes by direct global -> LDS loads into a ring of one or
+// two stages that belongs to the wavefront alone: nothing but its own count of outstanding loads is waited for.  (Loads straight into the
 // registers of the matrix instruction have 16 rows in 16 neighbouring lanes, four cache lines to every four lanes: 41 cache accesses
 // an instruction; one token through 8192 x 8192 weights of 4 bits took 12.6 us with the same bytes in flight, 11.7 with fewer.)
 //
@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(NW * 64) linear_mx_stream_kernel(LinearMxArgs 
     static_assert(NST * L < 64, "outstanding loads fit the counter");
     constexpr int kPad = F + 4;                          // floats between tokens of the partial sums
     static_assert(T * kPad * 4 <= NST * kStage, "partial sums in the wavefront's own stages");
-    extern __shared__ char lds[];                        // NW rings of two stages
+    extern __shared__ char lds[];                        // NW rings of NST stages
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, g = lane >> 4;

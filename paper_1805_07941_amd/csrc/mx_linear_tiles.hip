@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) linear_mx_tiles_kernel(Tile
     if constexpr (WHOLE) {
         // Small tiles: a step's operands are read while the step before it is multiplied, into the other of two sets, a few reads and
         // loads behind every matrix instruction (in blocks of reads, loads and products, which the wavefronts go through in step:
-        // 256 x 4096 x 4096 on 8 by 4 bits a tenth more time).
+        // 256 x 4096 x 4096 on 8 by 4 bits, aligned, a tenth more time).
         struct Set {
             Frag32<EW, EXACT> w[KK][TN];
             Frag32<EX, EXACT> x[KK][TM];
