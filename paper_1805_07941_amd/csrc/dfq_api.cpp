@@ -1270,7 +1270,7 @@ const CallEntry kCalls[] = {
     DFQ_ENTRY(dfq_eltwise_q), DFQ_ENTRY(dfq_concat_q_into), DFQ_ENTRY(dfq_pool_q), DFQ_ENTRY(dfq_quantize_np), DFQ_ENTRY(dfq_dequantize_np),
     DFQ_ENTRY(dfq_np_digits), DFQ_ENTRY(dfq_conv_np), DFQ_ENTRY(dfq_conv_np_add), DFQ_ENTRY(dfq_eltwise_np), DFQ_ENTRY(dfq_pool_np),
     DFQ_ENTRY(dfq_stem_pack_x), DFQ_ENTRY(dfq_quantize_mx), DFQ_ENTRY(dfq_dequantize_mx), DFQ_ENTRY(dfq_linear_mx), DFQ_ENTRY(dfq_linear_mx_q),
-    DFQ_ENTRY(dfq_linear_mx_variant),    DFQ_ENTRY(dfq_rms_norm_mx)};
+    DFQ_ENTRY(dfq_linear_mx_variant), DFQ_ENTRY(dfq_rms_norm_mx)};
 #undef DFQ_ENTRY
 constexpr int kNumCalls = (int)(sizeof(kCalls) / sizeof(kCalls[0]));
 
